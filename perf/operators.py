@@ -65,7 +65,19 @@ def _log_int(rng, lo, hi, step=1):
 
 
 def draw(rng):
-    """One more case: any of the operators, sizes over the listed cases' ranges."""
+    """One more case, of no more work than the largest listed one."""
+    most = max(work(c)["flops"] for c in listed())
+    c = _draw(rng)
+    while work(c)["flops"] > most:
+        c["tokens"] = (c["tokens"] + 1) // 2
+        c["padded"] = c.get("padded", 0) // 2
+    if c["op"] != "experts":
+        c.pop("padded", None)
+    return c
+
+
+def _draw(rng):
+    """Any of the operators, sizes over the listed cases' ranges."""
     op = rng.choice(["quantize", "gemm", "gemm", "route", "experts", "experts"])
     if op == "quantize":
         if rng.random() < 0.3:
