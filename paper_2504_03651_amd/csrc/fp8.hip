@@ -1,0 +1,226 @@
+// fp8.hip -- e4m3 quantisation and products (include/echo_fp8.h) for gfx950.
+#include <hip/hip_runtime.h>
+
+#include "echo_fp8.h"
+#include "fp8.hpp"
+#include "fp8_stream.hpp"
+#include "status.hpp"
+
+namespace echo {
+namespace fp8 {
+
+// ----------------------------------------------------------- quantisation
+
+// Eight values of x at element e, as fp32
+template <bool F32>
+__device__ __forceinline__ void load8(const void *x, int64_t e, float (&v)[8]) {
+    if constexpr (F32) {
+        const f32x4 a = ((const f32x4 *)((const float *)x + e))[0];
+        const f32x4 b = ((const f32x4 *)((const float *)x + e))[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    } else {
+        const u32x4 a = *(const u32x4 *)((const uint16_t *)x + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = bf2f(a[i] & 0xFFFFu), v[2 * i + 1] = bf2f(a[i] >> 16);
+    }
+}
+
+__device__ __forceinline__ float amax8(const float (&v)[8]) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));   // a NaN keeps out
+    return m;
+}
+
+__device__ __forceinline__ u32x2 codes8(const float (&v)[8], float s) {
+    u32x2 q;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        q[i] = e4m3x2(v[4 * i] / s, v[4 * i + 1] / s) |
+               (e4m3x2(v[4 * i + 2] / s, v[4 * i + 3] / s) << 16);
+    return q;
+}
+
+// Blocks of 1 x 128: 16 lanes a block, 8 values a lane.
+template <bool F32>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const void *x, int64_t stride,
+                                                            int64_t blocks, int cols, int cb,
+                                                            uint8_t *codes, float *scales) {
+    const int64_t b = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (b >= blocks) return;
+    const int64_t row = b / cb;
+    const int j = (int)(b - row * cb), col = kQ * j + 8 * (threadIdx.x & 15);
+    float v[8] = {};
+    if (col < cols) load8<F32>(x, row * stride + col, v);   // cols a multiple of 16
+    float m = amax8(v);
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    const float s = scale_of(m);
+    if ((threadIdx.x & 15) == 0) scales[b] = s;
+    if (col < cols) *(u32x2 *)(codes + row * cols + col) = codes8(v, s);
+}
+
+// Blocks of 128 x 128, one workgroup each: thread i has columns 8 (i % 16) ..
+// of rows i / 16, i / 16 + 16, ...
+template <bool F32>
+__global__ __launch_bounds__(256) void quantize_blocks_kernel(const void *x, int64_t stride,
+                                                              int rows, int cols, int rb, int cb,
+                                                              uint8_t *codes, float *scales) {
+    const int64_t b = blockIdx.x, mr = b / cb;   // matrix and row of blocks
+    const int64_t mat = mr / rb;
+    const int j = (int)(b - mr * cb), i = (int)(mr - mat * rb);
+    const int col = kQ * j + 8 * (threadIdx.x & 15);
+    const int row = kQ * i + (threadIdx.x >> 4);
+    float v[8][8] = {};
+    float m = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        if (col < cols && row + 16 * r < rows)
+            load8<F32>(x, (mat * rows + row + 16 * r) * stride + col, v[r]);
+        m = fmaxf(m, amax8(v[r]));
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    __shared__ float part[4];
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    const float s = scale_of(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
+    if (threadIdx.x == 0) scales[b] = s;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        if (col < cols && row + 16 * r < rows)
+            *(u32x2 *)(codes + (mat * rows + row + 16 * r) * (int64_t)cols + col) = codes8(v[r], s);
+}
+
+// -------------------------------------------------------------- products
+
+template <bool F32>
+void launch_gemm(const ProductArgs &p, hipStream_t st) {
+    const int tt = p.T > 48 ? 4 : p.T > 32 ? 3 : p.T > 16 ? 2 : 1;
+    const int n_tiles = cdiv(p.N, 16);
+    const dim3 grid((unsigned)(n_tiles * (int64_t)cdiv(p.T, 16 * tt))), block(256);
+    switch (tt) {
+        case 1: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 1, 4>), grid, block, 0, st, p, n_tiles); break;
+        case 2: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 2, 4>), grid, block, 0, st, p, n_tiles); break;
+        case 3: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 3, 4>), grid, block, 0, st, p, n_tiles); break;
+        default: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 4, 4>), grid, block, 0, st, p, n_tiles); break;
+    }
+}
+
+}  // namespace fp8
+}  // namespace echo
+
+using namespace echo;
+using namespace echo::fp8;
+
+namespace {
+
+int launched(const char *what) {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? ECHO_OK : fail(ECHO_E_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+int check_sizes(int32_t T, int32_t N, int32_t K) {
+    if (T < 0) return fail(ECHO_E_INVALID, "num_tokens %d", T);
+    if (N <= 0 || K <= 0) return fail(ECHO_E_INVALID, "out_features %d, in_features %d", N, K);
+    if (K % 16) return fail(ECHO_E_UNSUPPORTED, "in_features %d is not a multiple of 16", K);
+    if ((int64_t)cdiv(N, 16) * cdiv(T, 16) > INT32_MAX)
+        return fail(ECHO_E_UNSUPPORTED, "product of %d x %d too large", T, N);
+    return ECHO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int echo_fp8_quantize(const void *x, int32_t x_dtype, int64_t x_stride, int32_t batch,
+                      int32_t rows, int32_t cols, int32_t block_rows, void *codes, float *scales,
+                      void *stream) {
+    clear_error();
+    if (x_dtype != ECHO_BF16 && x_dtype != ECHO_F32)
+        return fail(ECHO_E_UNSUPPORTED, "dtype %d of x", x_dtype);
+    if (batch < 0 || rows < 0 || cols <= 0)
+        return fail(ECHO_E_INVALID, "batch %d, rows %d, cols %d", batch, rows, cols);
+    if (block_rows != 1 && block_rows != kQ)
+        return fail(ECHO_E_UNSUPPORTED, "block_rows %d (only 1, 128)", block_rows);
+    if (cols % 16) return fail(ECHO_E_UNSUPPORTED, "cols %d is not a multiple of 16", cols);
+    if (batch == 0 || rows == 0) return ECHO_OK;
+    const int size = x_dtype == ECHO_F32 ? 4 : 2;
+    if (!x || !codes || !scales) return fail(ECHO_E_INVALID, "x, codes or scales is NULL");
+    if (x_stride < cols || x_stride % (16 / size))
+        return fail(ECHO_E_INVALID, "x_stride %lld: at least cols %d, rows at 16-byte steps",
+                    (long long)x_stride, cols);
+    if (((uintptr_t)x | (uintptr_t)codes) & 15u)
+        return fail(ECHO_E_INVALID, "x and codes must be 16-byte aligned");
+    if ((uintptr_t)scales & 3u) return fail(ECHO_E_INVALID, "scales must be 4-byte aligned");
+    const int cb = cdiv(cols, kQ), rb = cdiv(rows, block_rows);
+    const hipStream_t st = (hipStream_t)stream;
+    const int64_t blocks = (int64_t)batch * rb * cb;
+    const int64_t grid = block_rows == 1 ? (blocks + 15) / 16 : blocks;
+    if (grid > INT32_MAX) return fail(ECHO_E_UNSUPPORTED, "%lld blocks", (long long)blocks);
+    if (block_rows == 1) {
+        if (size == 4)
+            hipLaunchKernelGGL(quantize_rows_kernel<true>, dim3((unsigned)grid), dim3(256), 0, st, x,
+                               x_stride, blocks, cols, cb, (uint8_t *)codes, scales);
+        else
+            hipLaunchKernelGGL(quantize_rows_kernel<false>, dim3((unsigned)grid), dim3(256), 0, st, x,
+                               x_stride, blocks, cols, cb, (uint8_t *)codes, scales);
+    } else {
+        if (size == 4)
+            hipLaunchKernelGGL(quantize_blocks_kernel<true>, dim3((unsigned)grid), dim3(256), 0, st,
+                               x, x_stride, rows, cols, rb, cb, (uint8_t *)codes, scales);
+        else
+            hipLaunchKernelGGL(quantize_blocks_kernel<false>, dim3((unsigned)grid), dim3(256), 0, st,
+                               x, x_stride, rows, cols, rb, cb, (uint8_t *)codes, scales);
+    }
+    return launched("echo_fp8_quantize");
+}
+
+size_t echo_fp8_gemm_workspace_bytes(int32_t num_tokens, int32_t out_features,
+                                     int32_t in_features) {
+    clear_error();
+    (void)check_sizes(num_tokens, out_features, in_features);
+    return 0;
+}
+
+int echo_fp8_gemm(const void *x, const float *x_scale, const void *w, const float *w_scale,
+                  int32_t num_tokens, int32_t out_features, int32_t in_features,
+                  const void *residual, void *y, int32_t y_dtype, int64_t y_stride,
+                  void *workspace, size_t workspace_bytes, void *stream) {
+    clear_error();
+    const int rc = check_sizes(num_tokens, out_features, in_features);
+    if (rc) return rc;
+    if (y_dtype != ECHO_BF16 && y_dtype != ECHO_F32)
+        return fail(ECHO_E_UNSUPPORTED, "dtype %d of y", y_dtype);
+    if (num_tokens == 0) return ECHO_OK;
+    if (!x || !x_scale || !w || !w_scale || !y)
+        return fail(ECHO_E_INVALID, "x, w, their scales or y is NULL");
+    if (y_stride < out_features)
+        return fail(ECHO_E_INVALID, "y_stride %lld < out_features %d", (long long)y_stride,
+                    out_features);
+    if (((uintptr_t)x | (uintptr_t)w) & 15u)
+        return fail(ECHO_E_INVALID, "x and w must be 16-byte aligned");
+    const uintptr_t ya = (uintptr_t)y | (uintptr_t)residual;
+    if (((uintptr_t)x_scale | (uintptr_t)w_scale) & 3u || ya & (y_dtype == ECHO_F32 ? 3u : 1u))
+        return fail(ECHO_E_INVALID, "scales, y and residual must have their types' alignment");
+    (void)workspace;
+    (void)workspace_bytes;
+    ProductArgs p{};
+    p.x = (const uint8_t *)x;
+    p.xs = x_scale;
+    p.w = (const uint8_t *)w;
+    p.ws = w_scale;
+    p.T = num_tokens;
+    p.N = out_features;
+    p.K = in_features;
+    p.KB = cdiv(in_features, kQ);
+    p.residual = residual;
+    p.y = y;
+    p.y_stride = y_stride;
+    if (y_dtype == ECHO_F32) launch_gemm<true>(p, (hipStream_t)stream);
+    else launch_gemm<false>(p, (hipStream_t)stream);
+    return launched("echo_fp8_gemm");
+}
+
+}  // extern "C"

@@ -1,0 +1,121 @@
+// fp8.hpp -- device pieces shared by the e4m3 kernels (fp8.hip, moe.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace echo {
+namespace fp8 {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kQ = 128;   // values of a row under one scale
+
+__host__ __device__ inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+__device__ __forceinline__ float bf2f(uint32_t b) { return __uint_as_float(b << 16); }
+
+// fp32 -> bf16, round to nearest even (NaN stays a quiet NaN)
+__device__ __forceinline__ uint32_t f2bf(float x) {
+    const uint32_t u = __float_as_uint(x);
+    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0x7FC0;
+    return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+}
+
+// Two fp32 -> two e4m3fn codes in the low 16 bits, round to nearest even,
+// saturating at 448, NaN to 0x7F (v_cvt_pk_fp8_f32 on clamped values).
+__device__ __forceinline__ uint32_t e4m3x2(float x, float y) {
+    const uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(
+        __builtin_amdgcn_fmed3f(x, -448.f, 448.f), __builtin_amdgcn_fmed3f(y, -448.f, 448.f), 0, false);
+    const uint32_t nan = (x != x ? 0x7Fu : 0u) | (y != y ? 0x7F00u : 0u);
+    const uint32_t keep = (x != x ? 0u : 0xFFu) | (y != y ? 0u : 0xFF00u);
+    return (w & keep) | nan;
+}
+
+// The scale of a block whose largest magnitude is amax
+__device__ __forceinline__ float scale_of(float amax) {
+    const float s = amax / 448.0f;
+    return s == 0.f ? 1.f : s;
+}
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// Eight e4m3 codes as bf16, exact (every e4m3 value is a bf16 value)
+__device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)lo, 1.0f, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)lo, 1.0f, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)hi, 1.0f, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)hi, 1.0f, true);
+    return (bf16x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// P[16 rows of a][16 rows of b] of 128 contraction steps, from zero.  Each lane
+// holds 32 codes of row lane % 16 of each operand; which of the 128 steps they
+// are is free as long as both operands agree (here bytes 16 g .. and 64 + 16 g ..,
+// g = lane / 16, two 16-byte loads).  The lane gets column lane % 16 (a row of
+// b) and rows 4 g .. 4 g + 3 (of a).
+//
+// The e4m3 instruction adds its products at fewer bits than fp32 holds: over
+// 200 tiles of N(0, 1) operands a sum of 128 was 1.5e-5 off in the 2-norm, the
+// 16x16x32 form the same to the bit.  Under a result that is rounded to bf16
+// (2^-9) that is nothing; fp32 results (WIDE) take the products in bf16, where
+// they are exact and the sum is 1e-8 off, at half the rate.
+template <bool WIDE>
+__device__ __forceinline__ f32x4 mfma128(i32x8 a, i32x8 b) {
+    f32x4 z = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(a[2 * i], a[2 * i + 1]),
+                                                        widen8(b[2 * i], b[2 * i + 1]), z, 0, 0, 0);
+        return z;
+    }
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, z, 0, 0, 0, 0, 0, 0);
+}
+
+__device__ __forceinline__ i32x8 pair(u32x4 lo, u32x4 hi) {
+    return (i32x8){(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
+                   (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+
+// ---------------------------------------------------------------- products
+
+// What a product's kernel reads and writes.
+//   Plain   y[t][n] (+)= x[t] . w[n]
+//   GateUp  rows are (token, expert) pairs in order of expert; a tile's pair p
+//           reads token order[p] / top_k and writes codes and scales of row p of
+//           SiLU(x . w[n]) * (x . w[N + n]), n < N = I
+//   Down    pair p reads row p and writes row order[p] of y
+enum class Mode { Plain, GateUp, Down };
+
+struct Tile {
+    int expert, row0, rows, pad;
+};
+
+struct ProductArgs {
+    const uint8_t *x;      // codes [rows][K]
+    const float *xs;       // [rows][KB]
+    const uint8_t *w;      // codes of the first expert
+    const float *ws;
+    int64_t w_expert, ws_expert;   // elements from one expert to the next
+    int T, N, K, KB;
+    // Plain, Down
+    const void *residual;
+    void *y;
+    int64_t y_stride;
+    // GateUp
+    uint8_t *hc;           // [pairs][N]
+    float *hs;             // [pairs][ceil(N / 128)]
+    // GateUp, Down
+    const int *num_tiles;
+    const Tile *tiles;
+    const int *order;      // pair of each place
+    int top_k;
+};
+
+}  // namespace fp8
+}  // namespace echo

@@ -1,0 +1,411 @@
+// moe.hip -- routing to experts and their products (include/echo_moe.h), gfx950.
+#include <hip/hip_runtime.h>
+
+#include <float.h>
+#include <algorithm>
+#include <cmath>
+
+#include "echo_moe.h"
+#include "fp8.hpp"
+#include "fp8_stream.hpp"
+#include "status.hpp"
+
+namespace echo {
+namespace fp8 {
+
+constexpr int kMaxExperts = 512, kMaxTopK = 64, kMaxGroups = 64;
+
+// ---------------------------------------------------------------- routing
+
+struct RouteArgs {
+    const void *logits;
+    int64_t stride;
+    const float *bias;
+    int T, E, top_k, groups, top_groups, group_top;
+    bool renormalize;
+    float scale;
+    int32_t *ids;
+    float *weights;
+};
+
+// x before y in falling order of (value, -index)
+__device__ __forceinline__ bool ahead(double xv, int xi, double yv, int yi) {
+    return xv > yv || (xv == yv && xi < yi);
+}
+
+// One wave per token; lane l has experts l, l + 64, ...
+template <bool F32, bool SIGMOID, int PER>
+__global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
+    extern __shared__ double lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t t = (int64_t)blockIdx.x * 4 + wave;
+    const bool live = t < a.T;
+    double *row = lds + wave * (a.groups > 1 ? a.E + kMaxGroups : 0);
+    double score[PER], key[PER];
+    double top = -DBL_MAX;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = lane + 64 * i;
+        double z = -INFINITY;
+        if (live && e < a.E) {
+            const int64_t at = t * a.stride + e;
+            const float f = F32 ? ((const float *)a.logits)[at] : bf2f(((const uint16_t *)a.logits)[at]);
+            if (f > -INFINITY) z = fmin((double)f, (double)FLT_MAX);   // not for NaN
+        }
+        key[i] = z;
+        top = fmax(top, z);
+    }
+    if constexpr (SIGMOID) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) score[i] = key[i] == -INFINITY ? 0.0 : 1.0 / (1.0 + exp(-key[i]));
+    } else {
+        for (int o = 1; o < 64; o <<= 1) top = fmax(top, __shfl_xor(top, o));
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            score[i] = key[i] == -INFINITY ? 0.0 : exp(key[i] - top);
+            sum += score[i];
+        }
+        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) score[i] = sum > 0.0 ? score[i] / sum : 0.0;
+    }
+    if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = lane + 64 * i;
+            double k = key[i] == -INFINITY ? -INFINITY : score[i] + (double)a.bias[min(e, a.E - 1)];
+            if (!(k > -INFINITY)) k = -INFINITY;   // a NaN too
+            key[i] = fmin(k, DBL_MAX);
+        }
+    }
+    if (a.groups > 1) {
+        const int per = a.E / a.groups;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = lane + 64 * i;
+            // a sum of two is of scores
+            if (e < a.E) row[e] = a.group_top == 2 && !a.bias && key[i] > -INFINITY ? score[i] : key[i];
+        }
+        __syncthreads();
+        double v = -INFINITY;
+        if (lane < a.groups) {
+            double b1 = -INFINITY, b2 = -INFINITY;
+            for (int j = 0; j < per; ++j) {
+                const double k = row[lane * per + j];
+                if (k > b1) b2 = b1, b1 = k;
+                else if (k > b2) b2 = k;
+            }
+            v = a.group_top == 2 ? fmin(b1 + b2, DBL_MAX) : b1;
+        }
+        int rank = 0;
+        for (int j = 0; j < a.groups; ++j) rank += ahead(__shfl(v, j), j, v, lane);
+        __syncthreads();
+        if (lane < a.groups) row[a.E + lane] = rank < a.top_groups ? 1.0 : 0.0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = lane + 64 * i;
+            if (e < a.E && row[a.E + e / per] == 0.0) key[i] = -INFINITY;
+        }
+    }
+    double mine = 0.0, sum = 0.0;   // lane j: the score of the row's j-th expert
+    int id = -1;
+    for (int j = 0; j < a.top_k; ++j) {
+        double v = -INFINITY, sc = 0.0;
+        int at = 0x7FFFFFFF;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (key[i] > v) v = key[i], at = lane + 64 * i, sc = score[i];
+        for (int o = 1; o < 64; o <<= 1) {
+            const double ov = __shfl_xor(v, o), os = __shfl_xor(sc, o);
+            const int oa = __shfl_xor(at, o);
+            if (ahead(ov, oa, v, at)) v = ov, at = oa, sc = os;
+        }
+        if (v == -INFINITY) break;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (at == lane + 64 * i) key[i] = -INFINITY;
+        if (lane == j) id = at, mine = sc;
+        sum += sc;
+    }
+    if (live && lane < a.top_k) {
+        const double w = a.renormalize ? (sum > 0.0 ? mine / sum : 0.0) : mine;
+        a.ids[t * a.top_k + lane] = id;
+        a.weights[t * a.top_k + lane] = (float)(w * (double)a.scale);
+    }
+}
+
+template <bool F32, bool SIGMOID>
+void launch_route(const RouteArgs &a, hipStream_t st) {
+    const dim3 grid((unsigned)cdiv(a.T, 4)), block(256);
+    const size_t lds = a.groups > 1 ? 4 * (a.E + kMaxGroups) * sizeof(double) : 0;
+    if (a.E <= 64) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 1>), grid, block, lds, st, a);
+    else if (a.E <= 128) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 2>), grid, block, lds, st, a);
+    else if (a.E <= 256) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 4>), grid, block, lds, st, a);
+    else hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 8>), grid, block, lds, st, a);
+}
+
+// ------------------------------------------------------------ the experts
+
+// Sorts the pairs by expert and cuts each expert's into tiles of `tile` rows:
+// counts, their prefix sums, then every pair to its place.  One workgroup.  The
+// order inside an expert is the order of the atomics, which no result hangs on:
+// a pair's row is computed alone and ends at the pair's own place.
+__global__ __launch_bounds__(1024) void sort_pairs_kernel(const int32_t *ids, int R, int E, int tile,
+                                                          int *num_tiles, Tile *tiles, int *order) {
+    __shared__ int count[kMaxExperts], first[kMaxExperts + 1], tfirst[kMaxExperts + 1];
+    const int tid = threadIdx.x;
+    if (tid < kMaxExperts) count[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < R; i += 1024) {
+        const int e = ids[i];
+        if (e >= 0 && e < E) atomicAdd(&count[e], 1);
+    }
+    __syncthreads();
+    if (tid == 0) {
+        int f = 0, tf = 0;
+        for (int e = 0; e < E; ++e) {
+            first[e] = f;
+            tfirst[e] = tf;
+            f += count[e];
+            tf += (count[e] + tile - 1) / tile;
+        }
+        *num_tiles = tf;
+    }
+    __syncthreads();
+    if (tid < E) {
+        const int n = count[tid], f = first[tid];
+        for (int i = 0; i * tile < n; ++i)
+            tiles[tfirst[tid] + i] = Tile{tid, f + i * tile, min(tile, n - i * tile), 0};
+        count[tid] = f;
+    }
+    __syncthreads();
+    for (int i = tid; i < R; i += 1024) {
+        const int e = ids[i];
+        if (e >= 0 && e < E) order[atomicAdd(&count[e], 1)] = i;
+    }
+}
+
+// out[t] = residual[t] + sum_j weights[t][j] y[t][j], eight columns a thread
+__global__ __launch_bounds__(256) void combine_kernel(const uint16_t *y, const int32_t *ids,
+                                                      const float *weights, const uint16_t *residual,
+                                                      uint16_t *out, int64_t n8, int H, int E,
+                                                      int top_k) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n8) return;
+    const int64_t t = i / (H / 8);
+    const int h = 8 * (int)(i - t * (H / 8));
+    float v[8] = {};
+    for (int j = 0; j < top_k; ++j) {
+        const int64_t pair = t * top_k + j;
+        const int e = ids[pair];
+        if (e < 0 || e >= E) continue;
+        const float w = weights[pair];
+        const u32x4 q = *(const u32x4 *)(y + pair * H + h);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            v[2 * r] += w * bf2f(q[r] & 0xFFFFu);
+            v[2 * r + 1] += w * bf2f(q[r] >> 16);
+        }
+    }
+    if (residual) {
+        const u32x4 q = *(const u32x4 *)(residual + t * H + h);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[2 * r] += bf2f(q[r] & 0xFFFFu), v[2 * r + 1] += bf2f(q[r] >> 16);
+    }
+    u32x4 o;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] = f2bf(v[2 * r]) | (f2bf(v[2 * r + 1]) << 16);
+    *(u32x4 *)(out + t * H + h) = o;
+}
+
+}  // namespace fp8
+}  // namespace echo
+
+using namespace echo;
+using namespace echo::fp8;
+
+namespace {
+
+struct Ws {
+    int tile, max_tiles;   // rows of a tile, and the most tiles there can be
+    size_t num_tiles, tiles, order, hs, hc, y, total;
+};
+
+int plan_ws(const echo_experts_t *x, int32_t T, int32_t top_k, Ws *w) {
+    if (!x) return fail(ECHO_E_INVALID, "experts is NULL");
+    if (x->num_experts < 1 || x->num_experts > kMaxExperts)
+        return fail(ECHO_E_UNSUPPORTED, "num_experts %d (1..%d)", x->num_experts, kMaxExperts);
+    if (x->hidden <= 0 || x->intermediate <= 0)
+        return fail(ECHO_E_INVALID, "hidden %d, intermediate %d", x->hidden, x->intermediate);
+    if (x->hidden % 16 || x->intermediate % 16 || x->intermediate > INT32_MAX / 2)
+        return fail(ECHO_E_UNSUPPORTED, "hidden %d and intermediate %d must be multiples of 16",
+                    x->hidden, x->intermediate);
+    if (T < 0) return fail(ECHO_E_INVALID, "num_tokens %d", T);
+    if (top_k < 1 || top_k > kMaxTopK) return fail(ECHO_E_INVALID, "top_k %d (1..%d)", top_k, kMaxTopK);
+    const int64_t R = (int64_t)T * top_k;
+    if (R > 1 << 24) return fail(ECHO_E_UNSUPPORTED, "%lld pairs of token and expert", (long long)R);
+    const int E = x->num_experts;
+    // tiles of 64 pairs where experts get that many on average
+    w->tile = R > 32 * (int64_t)E ? 64 : R > 16 * (int64_t)E ? 32 : 16;
+    w->max_tiles = (int)(R / w->tile + std::min<int64_t>(E, R));
+    if ((int64_t)w->max_tiles * cdiv(x->hidden, 16) > INT32_MAX ||
+        (int64_t)w->max_tiles * cdiv(x->intermediate, 16) > INT32_MAX)
+        return fail(ECHO_E_UNSUPPORTED, "%lld pairs of token and expert", (long long)R);
+    size_t o = 0;
+    auto take = [&](size_t n) { const size_t at = o; o += (n + 255) / 256 * 256; return at; };
+    w->num_tiles = take(4);
+    w->tiles = take(sizeof(Tile) * w->max_tiles);
+    w->order = take(4 * R);
+    w->hs = take(4 * R * cdiv(x->intermediate, kQ));
+    w->hc = take(R * x->intermediate);
+    w->y = take(2 * R * x->hidden);
+    w->total = R ? o : 0;
+    return ECHO_OK;
+}
+
+int launched(const char *what) {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? ECHO_OK : fail(ECHO_E_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+template <int TT>
+int run_experts(const ProductArgs &gu, const ProductArgs &dn, int max_tiles, hipStream_t st) {
+    const int ib = cdiv(gu.N, kQ), hb = cdiv(dn.N, 16);
+    hipLaunchKernelGGL((stream_gate_up_kernel<TT>), dim3((unsigned)max_tiles * ib), dim3(512), 0, st,
+                       gu, ib);
+    int rc = launched("gate and up products");
+    if (rc) return rc;
+    hipLaunchKernelGGL((stream_kernel<Mode::Down, false, TT, 4>), dim3((unsigned)max_tiles * hb),
+                       dim3(256), 0, st, dn, hb);
+    return launched("down product");
+}
+
+}  // namespace
+
+extern "C" {
+
+int echo_moe_route(const echo_router_t *r, const void *logits, int32_t logits_dtype,
+                   int64_t logits_stride, int32_t num_tokens, const float *bias, int32_t *ids,
+                   float *weights, void *stream) {
+    clear_error();
+    if (!r) return fail(ECHO_E_INVALID, "router is NULL");
+    if (r->num_experts < 1 || r->num_experts > kMaxExperts)
+        return fail(ECHO_E_UNSUPPORTED, "num_experts %d (1..%d)", r->num_experts, kMaxExperts);
+    if (r->score != ECHO_SCORE_SOFTMAX && r->score != ECHO_SCORE_SIGMOID)
+        return fail(ECHO_E_UNSUPPORTED, "score %d", r->score);
+    if (r->num_groups < 1 || r->num_groups > kMaxGroups || r->num_experts % r->num_groups)
+        return fail(ECHO_E_INVALID, "num_groups %d of %d experts (1..%d, of equal size)",
+                    r->num_groups, r->num_experts, kMaxGroups);
+    const int per = r->num_experts / r->num_groups;
+    if (r->top_groups < 1 || r->top_groups > r->num_groups)
+        return fail(ECHO_E_INVALID, "top_groups %d of %d", r->top_groups, r->num_groups);
+    if (r->group_top < 1 || r->group_top > 2 || (r->num_groups > 1 && r->group_top > per))
+        return fail(ECHO_E_INVALID, "group_top %d of %d experts a group", r->group_top, per);
+    if (r->top_k < 1 || r->top_k > kMaxTopK || r->top_k > r->top_groups * per)
+        return fail(ECHO_E_INVALID, "top_k %d (1..%d, of %d experts)", r->top_k, kMaxTopK,
+                    r->top_groups * per);
+    if (!std::isfinite(r->scale)) return fail(ECHO_E_INVALID, "scale is not finite");
+    if (logits_dtype != ECHO_BF16 && logits_dtype != ECHO_F32)
+        return fail(ECHO_E_UNSUPPORTED, "dtype %d of logits", logits_dtype);
+    if (num_tokens < 0) return fail(ECHO_E_INVALID, "num_tokens %d", num_tokens);
+    if (num_tokens == 0) return ECHO_OK;
+    if (!logits || !ids || !weights) return fail(ECHO_E_INVALID, "logits, ids or weights is NULL");
+    if (logits_stride < r->num_experts)
+        return fail(ECHO_E_INVALID, "logits_stride %lld < num_experts %d", (long long)logits_stride,
+                    r->num_experts);
+    const bool f32 = logits_dtype == ECHO_F32;
+    if ((uintptr_t)logits & (f32 ? 3u : 1u) ||
+        ((uintptr_t)ids | (uintptr_t)weights | (uintptr_t)bias) & 3u)
+        return fail(ECHO_E_INVALID, "a buffer is not aligned to its type");
+    const RouteArgs a{logits, logits_stride, bias, num_tokens, r->num_experts, r->top_k,
+                      r->num_groups, r->top_groups, r->group_top, r->renormalize != 0, r->scale,
+                      ids, weights};
+    const hipStream_t st = (hipStream_t)stream;
+    const bool sg = r->score == ECHO_SCORE_SIGMOID;
+    if (f32) sg ? launch_route<true, true>(a, st) : launch_route<true, false>(a, st);
+    else sg ? launch_route<false, true>(a, st) : launch_route<false, false>(a, st);
+    return launched("echo_moe_route");
+}
+
+size_t echo_moe_experts_workspace_bytes(const echo_experts_t *experts, int32_t num_tokens,
+                                        int32_t top_k) {
+    clear_error();
+    Ws w;
+    return plan_ws(experts, num_tokens, top_k, &w) ? 0 : w.total;
+}
+
+int echo_moe_experts(const echo_experts_t *m, const void *x, const float *x_scale,
+                     int32_t num_tokens, int32_t top_k, const int32_t *ids, const float *weights,
+                     const void *residual, void *out, void *workspace, size_t workspace_bytes,
+                     void *stream) {
+    clear_error();
+    Ws w;
+    int rc = plan_ws(m, num_tokens, top_k, &w);
+    if (rc) return rc;
+    if (!m->w_gate_up || !m->gate_up_scale || !m->w_down || !m->down_scale)
+        return fail(ECHO_E_INVALID, "an expert weight or scale is NULL");
+    if (((uintptr_t)m->w_gate_up | (uintptr_t)m->w_down) & 15u)
+        return fail(ECHO_E_INVALID, "expert weights must be 16-byte aligned");
+    if (num_tokens == 0) return ECHO_OK;
+    if (!x || !x_scale || !ids || !weights || !out)
+        return fail(ECHO_E_INVALID, "x, x_scale, ids, weights or out is NULL");
+    if (((uintptr_t)x | (uintptr_t)out | (uintptr_t)residual) & 15u)
+        return fail(ECHO_E_INVALID, "x, residual and out must be 16-byte aligned");
+    if (((uintptr_t)x_scale | (uintptr_t)ids | (uintptr_t)weights | (uintptr_t)m->gate_up_scale |
+         (uintptr_t)m->down_scale) & 3u)
+        return fail(ECHO_E_INVALID, "a buffer is not aligned to its type");
+    if (!workspace || workspace_bytes < w.total || ((uintptr_t)workspace & 255u))
+        return fail(ECHO_E_WORKSPACE, "workspace of %zu bytes (need %zu, 256-byte aligned)",
+                    workspace_bytes, w.total);
+    const hipStream_t st = (hipStream_t)stream;
+    uint8_t *base = (uint8_t *)workspace;
+    const int E = m->num_experts, H = m->hidden, I = m->intermediate, R = num_tokens * top_k;
+    const int HB = cdiv(H, kQ), IB = cdiv(I, kQ);
+    hipLaunchKernelGGL(sort_pairs_kernel, dim3(1), dim3(1024), 0, st, ids, R, E, w.tile,
+                       (int *)(base + w.num_tiles), (Tile *)(base + w.tiles), (int *)(base + w.order));
+    if ((rc = launched("sorting of pairs"))) return rc;
+
+    ProductArgs gu{};
+    gu.x = (const uint8_t *)x;
+    gu.xs = x_scale;
+    gu.w = (const uint8_t *)m->w_gate_up;
+    gu.ws = m->gate_up_scale;
+    gu.w_expert = 2 * (int64_t)I * H;
+    gu.ws_expert = 2 * (int64_t)IB * HB;
+    gu.T = R;
+    gu.N = I;
+    gu.K = H;
+    gu.KB = HB;
+    gu.hc = base + w.hc;
+    gu.hs = (float *)(base + w.hs);
+    gu.num_tiles = (const int *)(base + w.num_tiles);
+    gu.tiles = (const Tile *)(base + w.tiles);
+    gu.order = (const int *)(base + w.order);
+    gu.top_k = top_k;
+    ProductArgs dn = gu;
+    dn.x = gu.hc;
+    dn.xs = gu.hs;
+    dn.w = (const uint8_t *)m->w_down;
+    dn.ws = m->down_scale;
+    dn.w_expert = (int64_t)H * I;
+    dn.ws_expert = (int64_t)HB * IB;
+    dn.N = H;
+    dn.K = I;
+    dn.KB = IB;
+    dn.y = base + w.y;
+    dn.y_stride = H;
+    rc = w.tile == 64 ? run_experts<4>(gu, dn, w.max_tiles, st)
+         : w.tile == 32 ? run_experts<2>(gu, dn, w.max_tiles, st)
+                        : run_experts<1>(gu, dn, w.max_tiles, st);
+    if (rc) return rc;
+    const int64_t n8 = (int64_t)num_tokens * H / 8;
+    if (n8 > 256 * (int64_t)INT32_MAX) return fail(ECHO_E_UNSUPPORTED, "output too large");
+    hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((n8 + 255) / 256)), dim3(256), 0, st,
+                       (const uint16_t *)(base + w.y), ids, weights, (const uint16_t *)residual,
+                       (uint16_t *)out, n8, H, E, top_k);
+    return launched("weighted sum");
+}
+
+}  // extern "C"
