@@ -1,9 +1,12 @@
 // fp8.hip -- e4m3 quantisation and products (include/echo_fp8.h) for gfx950.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
+
 #include "echo_fp8.h"
 #include "fp8.hpp"
 #include "fp8_stream.hpp"
+#include "fp8_tiled.hpp"
 #include "status.hpp"
 
 namespace echo {
@@ -96,16 +99,23 @@ __global__ __launch_bounds__(256) void quantize_blocks_kernel(const void *x, int
 // -------------------------------------------------------------- products
 
 template <bool F32>
-void launch_gemm(const ProductArgs &p, hipStream_t st) {
+hipError_t launch_gemm(const ProductArgs &p, hipStream_t st) {
+    if (p.T > 64) {
+        if constexpr (!F32)
+            if ((int64_t)cdiv(p.N, 256) * cdiv(p.T, 256) >= 256)
+                return launch_tiled<Mode::Plain, F32, 256, 256, 2, 4>(p, cdiv(p.T, 256), st);
+        return launch_tiled<Mode::Plain, F32, 128, 128, 2, 2>(p, cdiv(p.T, 128), st);
+    }
     const int tt = p.T > 48 ? 4 : p.T > 32 ? 3 : p.T > 16 ? 2 : 1;
     const int n_tiles = cdiv(p.N, 16);
-    const dim3 grid((unsigned)(n_tiles * (int64_t)cdiv(p.T, 16 * tt))), block(256);
+    const dim3 grid((unsigned)n_tiles), block(256);
     switch (tt) {
         case 1: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 1, 4>), grid, block, 0, st, p, n_tiles); break;
         case 2: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 2, 4>), grid, block, 0, st, p, n_tiles); break;
         case 3: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 3, 4>), grid, block, 0, st, p, n_tiles); break;
         default: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 4, 4>), grid, block, 0, st, p, n_tiles); break;
     }
+    return hipSuccess;
 }
 
 }  // namespace fp8
@@ -218,8 +228,10 @@ int echo_fp8_gemm(const void *x, const float *x_scale, const void *w, const floa
     p.residual = residual;
     p.y = y;
     p.y_stride = y_stride;
-    if (y_dtype == ECHO_F32) launch_gemm<true>(p, (hipStream_t)stream);
-    else launch_gemm<false>(p, (hipStream_t)stream);
+    p.wide = out_features % 4 == 0 && y_stride % 4 == 0 && !(ya & (y_dtype == ECHO_F32 ? 15u : 7u));
+    const hipError_t e = y_dtype == ECHO_F32 ? launch_gemm<true>(p, (hipStream_t)stream)
+                                             : launch_gemm<false>(p, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(ECHO_E_HIP, "echo_fp8_gemm: %s", hipGetErrorString(e));
     return launched("echo_fp8_gemm");
 }
 

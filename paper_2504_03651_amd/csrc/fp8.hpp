@@ -107,6 +107,7 @@ struct ProductArgs {
     const void *residual;
     void *y;
     int64_t y_stride;
+    bool wide;             // see store4
     // GateUp
     uint8_t *hc;           // [pairs][N]
     float *hs;             // [pairs][ceil(N / 128)]
@@ -116,6 +117,40 @@ struct ProductArgs {
     const int *order;      // pair of each place
     int top_k;
 };
+
+// y of a lane's four columns n .. n + 3 of row t, the residual added; p.wide:
+// N and y_stride multiples of 4, y and residual aligned to four values
+template <bool F32>
+__device__ __forceinline__ void store4(const ProductArgs &p, int64_t t, int n, f32x4 v) {
+    const int64_t at = t * p.y_stride + n;
+    if (p.wide) {
+        if (n >= p.N) return;
+        if constexpr (F32) {
+            if (p.residual) v += *(const f32x4 *)((const float *)p.residual + at);
+            *(f32x4 *)((float *)p.y + at) = v;
+        } else {
+            if (p.residual) {
+                const u32x2 q = *(const u32x2 *)((const uint16_t *)p.residual + at);
+#pragma unroll
+                for (int r = 0; r < 2; ++r) v[2 * r] += bf2f(q[r] & 0xFFFFu), v[2 * r + 1] += bf2f(q[r] >> 16);
+            }
+            *(u32x2 *)((uint16_t *)p.y + at) =
+                (u32x2){f2bf(v[0]) | (f2bf(v[1]) << 16), f2bf(v[2]) | (f2bf(v[3]) << 16)};
+        }
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        if (n + r >= p.N) return;
+        if constexpr (F32) {
+            if (p.residual) v[r] += ((const float *)p.residual)[at + r];
+            ((float *)p.y)[at + r] = v[r];
+        } else {
+            if (p.residual) v[r] += bf2f(((const uint16_t *)p.residual)[at + r]);
+            ((uint16_t *)p.y)[at + r] = (uint16_t)f2bf(v[r]);
+        }
+    }
+}
 
 }  // namespace fp8
 }  // namespace echo

@@ -56,23 +56,6 @@ __device__ __forceinline__ void stream_blocks(const uint8_t *const (&w)[NT],
     }
 }
 
-// y of a lane's four columns n .. n + 3 of row t
-template <bool F32>
-__device__ __forceinline__ void store4(const ProductArgs &p, int64_t t, int n, f32x4 v) {
-    const int64_t at = t * p.y_stride + n;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        if (n + r >= p.N) return;
-        if constexpr (F32) {
-            if (p.residual) v[r] += ((const float *)p.residual)[at + r];
-            ((float *)p.y)[at + r] = v[r];
-        } else {
-            if (p.residual) v[r] += bf2f(((const uint16_t *)p.residual)[at + r]);
-            ((uint16_t *)p.y)[at + r] = (uint16_t)f2bf(v[r]);
-        }
-    }
-}
-
 // One workgroup: 16 weight rows, 16 TT tokens, its KS waves taking every KS-th
 // block of K; their sums meet in LDS in the waves' order.
 template <Mode M, bool F32, int TT, int KS>

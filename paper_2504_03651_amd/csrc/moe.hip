@@ -3,11 +3,13 @@
 
 #include <float.h>
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "echo_moe.h"
 #include "fp8.hpp"
 #include "fp8_stream.hpp"
+#include "fp8_tiled.hpp"
 #include "status.hpp"
 
 namespace echo {
@@ -36,11 +38,11 @@ __device__ __forceinline__ bool ahead(double xv, int xi, double yv, int yi) {
 // One wave per token; lane l has experts l, l + 64, ...
 template <bool F32, bool SIGMOID, int PER>
 __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
-    extern __shared__ double lds[];
+    extern __shared__ double route_lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t t = (int64_t)blockIdx.x * 4 + wave;
     const bool live = t < a.T;
-    double *row = lds + wave * (a.groups > 1 ? a.E + kMaxGroups : 0);
+    double *row = route_lds + wave * (a.groups > 1 ? a.E + kMaxGroups : 0);
     double score[PER], key[PER];
     double top = -DBL_MAX;
 #pragma unroll
@@ -247,8 +249,9 @@ int plan_ws(const echo_experts_t *x, int32_t T, int32_t top_k, Ws *w) {
     const int64_t R = (int64_t)T * top_k;
     if (R > 1 << 24) return fail(ECHO_E_UNSUPPORTED, "%lld pairs of token and expert", (long long)R);
     const int E = x->num_experts;
-    // tiles of 64 pairs where experts get that many on average
-    w->tile = R > 32 * (int64_t)E ? 64 : R > 16 * (int64_t)E ? 32 : 16;
+    // tiles of as many pairs as experts get on average
+    const int64_t mean = R / E;
+    w->tile = mean > 128 ? 256 : mean > 32 ? 64 : mean > 16 ? 32 : 16;
     w->max_tiles = (int)(R / w->tile + std::min<int64_t>(E, R));
     if ((int64_t)w->max_tiles * cdiv(x->hidden, 16) > INT32_MAX ||
         (int64_t)w->max_tiles * cdiv(x->intermediate, 16) > INT32_MAX)
@@ -271,15 +274,23 @@ int launched(const char *what) {
 }
 
 template <int TT>
-int run_experts(const ProductArgs &gu, const ProductArgs &dn, int max_tiles, hipStream_t st) {
+hipError_t stream_experts(const ProductArgs &gu, const ProductArgs &dn, int max_tiles, hipStream_t st) {
     const int ib = cdiv(gu.N, kQ), hb = cdiv(dn.N, 16);
     hipLaunchKernelGGL((stream_gate_up_kernel<TT>), dim3((unsigned)max_tiles * ib), dim3(512), 0, st,
                        gu, ib);
-    int rc = launched("gate and up products");
-    if (rc) return rc;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL((stream_kernel<Mode::Down, false, TT, 4>), dim3((unsigned)max_tiles * hb),
                        dim3(256), 0, st, dn, hb);
-    return launched("down product");
+    return hipSuccess;
+}
+
+template <int BT, int WN, int WT>
+hipError_t tiled_experts(const ProductArgs &gu, const ProductArgs &dn, int max_tiles, hipStream_t st) {
+    hipError_t e = launch_tiled<Mode::GateUp, false, 256, BT, WN, WT>(gu, max_tiles, st);
+    if (e == hipSuccess) e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return launch_tiled<Mode::Down, false, 256, BT, WN, WT>(dn, max_tiles, st);
 }
 
 }  // namespace
@@ -396,10 +407,13 @@ int echo_moe_experts(const echo_experts_t *m, const void *x, const float *x_scal
     dn.KB = IB;
     dn.y = base + w.y;
     dn.y_stride = H;
-    rc = w.tile == 64 ? run_experts<4>(gu, dn, w.max_tiles, st)
-         : w.tile == 32 ? run_experts<2>(gu, dn, w.max_tiles, st)
-                        : run_experts<1>(gu, dn, w.max_tiles, st);
-    if (rc) return rc;
+    dn.wide = true;   // H a multiple of 16, y the workspace's
+    const hipError_t e = w.tile == 256  ? tiled_experts<256, 2, 4>(gu, dn, w.max_tiles, st)
+                         : w.tile == 64 ? tiled_experts<64, 4, 1>(gu, dn, w.max_tiles, st)
+                         : w.tile == 32 ? stream_experts<2>(gu, dn, w.max_tiles, st)
+                                        : stream_experts<1>(gu, dn, w.max_tiles, st);
+    if (e != hipSuccess) return fail(ECHO_E_HIP, "experts' products: %s", hipGetErrorString(e));
+    if ((rc = launched("experts' products"))) return rc;
     const int64_t n8 = (int64_t)num_tokens * H / 8;
     if (n8 > 256 * (int64_t)INT32_MAX) return fail(ECHO_E_UNSUPPORTED, "output too large");
     hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((n8 + 255) / 256)), dim3(256), 0, st,
