@@ -1,6 +1,7 @@
 // fp8.hip -- e4m3 quantisation and products (include/echo_fp8.h) for gfx950.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "echo_fp8.h"
@@ -98,23 +99,103 @@ __global__ __launch_bounds__(256) void quantize_blocks_kernel(const void *x, int
 
 // -------------------------------------------------------------- products
 
+// y = the sum of the parts of all ranges of K (+ residual), four columns a thread
 template <bool F32>
-hipError_t launch_gemm(const ProductArgs &p, hipStream_t st) {
-    if (p.T > 64) {
-        if constexpr (!F32)
-            if ((int64_t)cdiv(p.N, 256) * cdiv(p.T, 256) >= 256)
-                return launch_tiled<Mode::Plain, F32, 256, 256, 2, 4>(p, cdiv(p.T, 256), st);
-        return launch_tiled<Mode::Plain, F32, 128, 128, 2, 2>(p, cdiv(p.T, 128), st);
+__global__ __launch_bounds__(256) void add_parts_kernel(ProductArgs p, int splits) {
+    const int q = p.part_pitch / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)p.T * q) return;
+    const int64_t t = i / q;
+    const int n = 4 * (int)(i - t * q);
+    f32x4 v = *(const f32x4 *)(p.part + t * p.part_pitch + n);
+    for (int s = 1; s < splits; ++s) v += *(const f32x4 *)(p.part + (s * (int64_t)p.T + t) * p.part_pitch + n);
+    store4<F32>(p, t, n, v);
+}
+
+// How a product is cut: the kernel's form, and how many ranges of K there are.
+enum Form { kRows16, kRows32, k64x32, k64x64, k128x64, k128x128, k256x128, k256x256 };
+struct Cut {
+    Form form;
+    int splits;
+};
+
+// The cut of least estimated time, in microseconds fitted to 130 sizes (T 1 to
+// 4,640, N x K from 512 x 512 to 28672 x 4096, weights from memory); the cuts it
+// takes there cost 4% over the best of 21 forms x 8 splits in the geometric mean.
+//   A launch is 3.4.  Weights and tokens come at 5.2 TB/s at most.
+//   kRows: 16 or 32 weight rows a workgroup, straight into registers; a CU streams
+//   20 KB a microsecond, and less the more tokens' codes come beside them (8 x
+//   6144 x 4096: 10.2 by 32 rows, 12.1 by 16; x 4096 x 4096: 9.9 and 7.7).
+//   Tiles n x t: what a step of 128 of K takes with one workgroup on a CU, and
+//   with two where LDS holds two.
+//   Ranges of K cost a second launch and their fp32 parts' way to memory and back
+//   (137 x 4096 x 14336: 95 in one range, 30.7 to 32 in eight).
+Cut cut_of(int T, int N, int K) {
+    const int KB = cdiv(K, kQ);
+    const double bytes = (double)N * K + (double)T * K;
+    Cut best{kRows16, 1};
+    double least = 1e30;
+    for (int nt = 1; nt <= 2; ++nt) {
+        const int64_t wgs = (int64_t)cdiv(N, 16 * nt) * cdiv(T, 32);
+        const double turn = 16.0 * nt * K / 20e3 * (1 + 0.035 * std::min(T, 32) / nt);
+        const double us = std::max(bytes / 5.2e6, turn * (1 + 0.6 * ((double)((wgs + 255) / 256) - 1)));
+        if (us < least) least = us, best = Cut{nt == 1 ? kRows16 : kRows32, 1};
     }
-    const int tt = p.T > 48 ? 4 : p.T > 32 ? 3 : p.T > 16 ? 2 : 1;
-    const int n_tiles = cdiv(p.N, 16);
-    const dim3 grid((unsigned)n_tiles), block(256);
-    switch (tt) {
-        case 1: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 1, 4>), grid, block, 0, st, p, n_tiles); break;
-        case 2: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 2, 4>), grid, block, 0, st, p, n_tiles); break;
-        case 3: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 3, 4>), grid, block, 0, st, p, n_tiles); break;
-        default: hipLaunchKernelGGL((stream_kernel<Mode::Plain, F32, 4, 4>), grid, block, 0, st, p, n_tiles); break;
+    static const struct {
+        Form form;
+        int n, t;
+        double one, two;
+    } tiles[] = {{k64x32, 64, 32, .37, .52},   {k64x64, 64, 64, .45, .75}, {k128x64, 128, 64, .68, 1.0},
+                 {k128x128, 128, 128, .88, 0}, {k256x128, 256, 128, 1.32, 0}, {k256x256, 256, 256, 2.4, 0}};
+    for (const auto &f : tiles) {
+        if (f.t > 32 && T <= f.t / 2) continue;
+        for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (s > 1 && 2 * s > KB) break;
+            const int64_t each = ((int64_t)cdiv(N, f.n) * cdiv(T, f.t) * s + 255) / 256;   // of a CU
+            const double turns = f.two > 0 ? (double)(each / 2) * f.two + (double)(each % 2) * f.one
+                                           : (double)each * f.one;
+            const double starts = (double)(f.two > 0 ? (each + 1) / 2 : each) - 1;
+            double us = std::max(cdiv(KB, s) * turns + 2.5 * starts, bytes / 5.2e6);
+            if (s > 1) us += 3.4 + 0.25 * s + 8.0 * s * T * N / 5e6;
+            if (us < least) least = us, best = Cut{f.form, s};
+        }
     }
+    return best;
+}
+
+template <bool F32, int NT, int TT>
+void launch_rows(const ProductArgs &p, hipStream_t st) {
+    const int n_tiles = cdiv(p.N, 16 * NT);
+    const dim3 grid((unsigned)((int64_t)n_tiles * cdiv(p.T, 16 * TT))), block(512);
+    if (p.T <= 16 * TT)   // every weight read once
+        hipLaunchKernelGGL((stream_kernel<F32, true, NT, TT, 8, 4>), grid, block, 0, st, p, n_tiles);
+    else
+        hipLaunchKernelGGL((stream_kernel<F32, false, NT, TT, 8, 4>), grid, block, 0, st, p, n_tiles);
+}
+
+template <bool F32, int BN, int BT, int WN, int WT, int S>
+hipError_t launch_tiles(const ProductArgs &p, int splits, hipStream_t st) {
+    return launch_tiled<Mode::Plain, F32, BN, BT, WN, WT, S>(p, cdiv(p.T, BT), splits, st);
+}
+
+template <bool F32>
+hipError_t launch_gemm(const ProductArgs &p, Cut c, hipStream_t st) {
+    hipError_t e = hipSuccess;
+    switch (c.form) {
+        case kRows16: p.T > 16 ? launch_rows<F32, 1, 2>(p, st) : launch_rows<F32, 1, 1>(p, st); return e;
+        case kRows32: p.T > 16 ? launch_rows<F32, 2, 2>(p, st) : launch_rows<F32, 2, 1>(p, st); return e;
+        case k64x32: e = launch_tiles<F32, 64, 32, 4, 1, 5>(p, c.splits, st); break;
+        case k64x64: e = launch_tiles<F32, 64, 64, 4, 1, 4>(p, c.splits, st); break;
+        case k128x64: e = launch_tiles<F32, 128, 64, 4, 1, 3>(p, c.splits, st); break;
+        default:
+            // fp32 results, which take twice the products, in tiles of 128 x 128
+            if (F32 || c.form == k128x128) e = launch_tiles<F32, 128, 128, 4, 2, 4>(p, c.splits, st);
+            else if (c.form == k256x128) e = launch_tiles<false, 256, 128, 4, 2, 3>(p, c.splits, st);
+            else e = launch_tiles<false, 256, 256, 2, 4, 2>(p, c.splits, st);
+    }
+    if (e != hipSuccess || c.splits == 1 || (e = hipGetLastError()) != hipSuccess) return e;
+    const int64_t n = (int64_t)p.T * (p.part_pitch / 4);
+    hipLaunchKernelGGL(add_parts_kernel<F32>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, p, c.splits);
     return hipSuccess;
 }
 
@@ -131,11 +212,20 @@ int launched(const char *what) {
     return e == hipSuccess ? ECHO_OK : fail(ECHO_E_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+// columns of a row of parts
+int pitch_of(int32_t N) { return (int)(((int64_t)N + 3) / 4 * 4); }
+
+size_t parts_bytes(Cut c, int32_t T, int32_t N) {
+    return c.splits == 1 ? 0 : (size_t)c.splits * T * pitch_of(N) * 4;
+}
+
 int check_sizes(int32_t T, int32_t N, int32_t K) {
     if (T < 0) return fail(ECHO_E_INVALID, "num_tokens %d", T);
     if (N <= 0 || K <= 0) return fail(ECHO_E_INVALID, "out_features %d, in_features %d", N, K);
     if (K % 16) return fail(ECHO_E_UNSUPPORTED, "in_features %d is not a multiple of 16", K);
-    if ((int64_t)cdiv(N, 16) * cdiv(T, 16) > INT32_MAX)
+    // offsets inside a tile are 32 bits, a grid's workgroups too
+    if (K > 1 << 23) return fail(ECHO_E_UNSUPPORTED, "in_features %d above %d", K, 1 << 23);
+    if ((int64_t)cdiv(N, 16) * cdiv(T, 16) > INT32_MAX / 2 || N > INT32_MAX - 3)
         return fail(ECHO_E_UNSUPPORTED, "product of %d x %d too large", T, N);
     return ECHO_OK;
 }
@@ -190,8 +280,8 @@ int echo_fp8_quantize(const void *x, int32_t x_dtype, int64_t x_stride, int32_t 
 size_t echo_fp8_gemm_workspace_bytes(int32_t num_tokens, int32_t out_features,
                                      int32_t in_features) {
     clear_error();
-    (void)check_sizes(num_tokens, out_features, in_features);
-    return 0;
+    if (check_sizes(num_tokens, out_features, in_features) || num_tokens == 0) return 0;
+    return parts_bytes(cut_of(num_tokens, out_features, in_features), num_tokens, out_features);
 }
 
 int echo_fp8_gemm(const void *x, const float *x_scale, const void *w, const float *w_scale,
@@ -214,8 +304,11 @@ int echo_fp8_gemm(const void *x, const float *x_scale, const void *w, const floa
     const uintptr_t ya = (uintptr_t)y | (uintptr_t)residual;
     if (((uintptr_t)x_scale | (uintptr_t)w_scale) & 3u || ya & (y_dtype == ECHO_F32 ? 3u : 1u))
         return fail(ECHO_E_INVALID, "scales, y and residual must have their types' alignment");
-    (void)workspace;
-    (void)workspace_bytes;
+    const Cut cut = cut_of(num_tokens, out_features, in_features);
+    const size_t need = parts_bytes(cut, num_tokens, out_features);
+    if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u)))
+        return fail(ECHO_E_WORKSPACE, "workspace of %zu bytes (need %zu, 256-byte aligned)",
+                    workspace_bytes, need);
     ProductArgs p{};
     p.x = (const uint8_t *)x;
     p.xs = x_scale;
@@ -228,9 +321,11 @@ int echo_fp8_gemm(const void *x, const float *x_scale, const void *w, const floa
     p.residual = residual;
     p.y = y;
     p.y_stride = y_stride;
+    p.part = (float *)workspace;
+    p.part_pitch = pitch_of(out_features);
     p.wide = out_features % 4 == 0 && y_stride % 4 == 0 && !(ya & (y_dtype == ECHO_F32 ? 15u : 7u));
-    const hipError_t e = y_dtype == ECHO_F32 ? launch_gemm<true>(p, (hipStream_t)stream)
-                                             : launch_gemm<false>(p, (hipStream_t)stream);
+    const hipError_t e = y_dtype == ECHO_F32 ? launch_gemm<true>(p, cut, (hipStream_t)stream)
+                                             : launch_gemm<false>(p, cut, (hipStream_t)stream);
     if (e != hipSuccess) return fail(ECHO_E_HIP, "echo_fp8_gemm: %s", hipGetErrorString(e));
     return launched("echo_fp8_gemm");
 }

@@ -108,6 +108,8 @@ struct ProductArgs {
     void *y;
     int64_t y_stride;
     bool wide;             // see store4
+    float *part;           // [splits][T][part_pitch], for products over ranges of K
+    int part_pitch;
     // GateUp
     uint8_t *hc;           // [pairs][N]
     float *hs;             // [pairs][ceil(N / 128)]

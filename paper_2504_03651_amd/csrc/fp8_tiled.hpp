@@ -11,29 +11,42 @@ typedef __attribute__((address_space(3))) void lds_void;
 // where 16-byte pieces past the end of a row come from
 __device__ __align__(16) const uint8_t kZeros[16] = {};
 
-// s_waitcnt immediate: vmcnt n, everything else unconstrained
-constexpr int wait_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
+// All but the last n of this wave's copies into LDS have landed and its reads of
+// LDS are done; then all waves'.
+template <int N>
+__device__ __forceinline__ void landed_but() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
 
 // One workgroup of WN x WT waves: BN weight rows (GateUp: BN / 2 gate rows and
-// the up rows of the same columns) by BT tokens, K in steps of 128 through two
-// LDS buffers that are filled straight from memory.  A row's 128 codes are eight
-// 16-byte pieces; piece q of row r lies at place q ^ (r & 7), so that the eight
-// lanes that read one piece of eight rows meet eight different places.  Each
-// step's sum comes out of the matrix instruction alone and is scaled on its way
-// into the accumulators: one FMA a value, beside the products of the next tiles.
-template <Mode M, bool F32, int BN, int BT, int WN, int WT>
-__global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n_tiles, int t_tiles) {
+// the up rows of the same columns) by BT tokens, K in steps of 128 through a ring
+// of S LDS stages that are filled straight from memory, S - 1 steps ahead.  A
+// row's 128 codes are eight 16-byte pieces; piece q of row r lies at place
+// q ^ (r & 7), so that the eight lanes that read one piece of eight rows meet
+// eight different places.  Behind a stage's codes lie each wave's scales: one of
+// each of its tokens, and one (GateUp: two) of its weight rows.  Each step's sum
+// comes out of the matrix instruction alone and is scaled on its way into the
+// accumulators, one FMA a value.
+// part: fp32 sums of one of `splits` equal ranges of K go to part[split][t][n],
+// rows part_pitch apart, instead of y.
+template <Mode M, bool F32, int BN, int BT, int WN, int WT, int S>
+__global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n_tiles, int splits) {
     constexpr int W = WN * WT, NW = BN / WN, TW = BT / WT;   // a wave's rows and tokens
     constexpr int NI = NW / 16, NJ = TW / 16;
-    constexpr int STAGE = (BN + BT) * kQ;
-    constexpr int COPIES = STAGE / 1024 / W;   // 1 KiB copies of a wave per step
-    static_assert(COPIES * 1024 * W == STAGE && NI >= 2);
+    constexpr int CODES = (BN + BT) * kQ, STAGE = CODES + 512 * W;
+    constexpr int PIECES = CODES / 1024;                     // 1 KiB copies of a stage
+    constexpr int COPIES = (PIECES + W - 1) / W, EXTRA = PIECES % W;
+    static_assert(NW % (M == Mode::GateUp ? 32 : 16) == 0 && TW % 16 == 0 && TW <= 64 && S >= 2);
     extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave % WN, wt = wave / WN;
 
-    const int ti = blockIdx.x / n_tiles, nb = blockIdx.x - ti * n_tiles;
+    int b = blockIdx.x;
+    const int split = b % splits;
+    b /= splits;
+    const int ti = b / n_tiles, nb = b - ti * n_tiles;
+    const int kb0 = (int)((int64_t)p.KB * split / splits), kb1 = (int)((int64_t)p.KB * (split + 1) / splits);
     int row0 = BT * ti, rows = min(BT, p.T - row0);
     const uint8_t *wbase = p.w;
     const float *sbase = p.ws;
@@ -47,57 +60,62 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
     }
     const int n0 = (M == Mode::GateUp ? BN / 2 : BN) * nb;
 
-    // sources of this lane's copies: rows of weights, then of tokens
-    const uint8_t *src[COPIES];
-#pragma unroll
-    for (int i = 0; i < COPIES; ++i) {
-        const int r = 8 * (wave * COPIES + i) + (lane >> 3);   // row of the stage
-        int64_t at;
-        if (r < BN) {
-            if constexpr (M == Mode::GateUp) {
-                const int q = r % NW, n = min(n0 + (r / NW) * (NW / 2) + q % (NW / 2), p.N - 1);
-                at = (int64_t)(q < NW / 2 ? n : p.N + n) * p.K;
-            } else {
-                at = (int64_t)min(n0 + r, p.N - 1) * p.K;
-            }
-            src[i] = wbase + at;
-        } else {
-            int64_t t = row0 + min(r - BN, rows - 1);
-            if constexpr (M == Mode::GateUp) t = p.order[t] / p.top_k;
-            src[i] = p.x + t * p.K;
-        }
+    // sources of this lane's copies, in bytes from the tile's weights (rows of
+    // the stage below BN) and from its tokens
+    const uint8_t *wsrc = wbase, *xsrc = p.x;
+    const float *xscale = p.xs;
+    if constexpr (M != Mode::GateUp) {
+        wsrc += (int64_t)n0 * p.K;
+        xsrc += (int64_t)row0 * p.K;
+        xscale += (int64_t)row0 * p.KB;
     }
     const int piece = (lane & 7) ^ (lane >> 3);
-    auto copy = [&](int kb, int buf) {
-        const int k = kQ * kb + 16 * piece;
-        uint8_t *dst = lds + buf * STAGE + wave * COPIES * 1024;
-        if (kQ * (kb + 1) <= p.K) {
-#pragma unroll
-            for (int i = 0; i < COPIES; ++i)
-                __builtin_amdgcn_global_load_lds((const void *)(src[i] + k), (lds_void *)(dst + 1024 * i), 16, 0, 0);
-        } else {
-#pragma unroll
-            for (int i = 0; i < COPIES; ++i)
-                __builtin_amdgcn_global_load_lds((const void *)(k < p.K ? src[i] + k : kZeros),
-                                                 (lds_void *)(dst + 1024 * i), 16, 0, 0);
-        }
+    auto token = [&](int r) -> uint32_t {   // row of x that the tile's row r reads
+        r = min(r, rows - 1);
+        return M == Mode::GateUp ? (uint32_t)(p.order[row0 + r] / p.top_k) : (uint32_t)r;
     };
-
-    // scales: one of each token column, one (GateUp: two) of the wave's weight rows
-    const float *xs[NJ];
+    // copies of a wave: COPIES, or one less where the stage's pieces run out
+    const bool more = EXTRA == 0 || wave < EXTRA;
+    uint32_t src[COPIES];
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-        int64_t t = row0 + min(wt * TW + 16 * j + c, rows - 1);
-        if constexpr (M == Mode::GateUp) t = p.order[t] / p.top_k;
-        xs[j] = p.xs + t * p.KB;
+    for (int i = 0; i < COPIES; ++i) {
+        const int r = min(8 * (W * i + wave), BN + BT - 8) + (lane >> 3);
+        uint32_t row;
+        if (W * i + wave >= BN / 8) {
+            row = token(r - BN);
+        } else if constexpr (M == Mode::GateUp) {
+            const int q = r % NW, n = min(n0 + (r / NW) * (NW / 2) + q % (NW / 2), p.N - 1);
+            row = q < NW / 2 ? n : p.N + n;
+        } else {
+            row = min(r, p.N - 1 - n0);
+        }
+        src[i] = row * (uint32_t)p.K + 16 * piece;
     }
-    const float *ws0, *ws1;
-    if constexpr (M == Mode::GateUp) {
-        ws0 = sbase + (int64_t)nb * p.KB;
-        ws1 = ws0 + (int64_t)n_tiles * p.KB;
-    } else {
-        ws0 = ws1 = sbase + (int64_t)min((n0 + wn * NW) / kQ, (p.N - 1) / kQ) * p.KB;
-    }
+    const uint32_t xs = token(wt * TW + lane % TW) * (uint32_t)p.KB;
+    const float *ws;   // lanes below 32: the (gate) rows' scales, above: the up rows'
+    if constexpr (M == Mode::GateUp) ws = sbase + (int64_t)(lane < 32 ? nb : n_tiles + nb) * p.KB;
+    else ws = sbase + (int64_t)min((n0 + wn * NW) / kQ, (p.N - 1) / kQ) * p.KB;
+    auto copy = [&](int kb, int slot) {
+        uint8_t *stage = lds + slot * STAGE, *dst = stage + 1024 * wave;
+        const uint8_t *w = wsrc + (int64_t)kQ * kb, *x = xsrc + (int64_t)kQ * kb;
+        const bool whole = kQ * (kb + 1) <= p.K, in = kQ * kb + 16 * piece < p.K;
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            if (i + 1 == COPIES && !more) break;
+            const uint8_t *from = (W * i + wave < BN / 8 ? w : x) + src[i];
+            __builtin_amdgcn_global_load_lds((const void *)(whole || in ? from : kZeros),
+                                             (lds_void *)(dst + 1024 * W * i), 16, 0, 0);
+        }
+        float *sc = (float *)(stage + CODES) + 128 * wave;
+        __builtin_amdgcn_global_load_lds((const void *)(xscale + kb + xs), (lds_void *)sc, 4, 0, 0);
+        __builtin_amdgcn_global_load_lds((const void *)(ws + kb), (lds_void *)(sc + 64), 4, 0, 0);
+    };
+    constexpr int AHEAD = S - 2;   // stages that may be in flight behind the next one
+    auto landed = [&](int kb) {
+        if (kb + AHEAD >= kb1 || AHEAD == 0) landed_but<0>();
+        else if (more) landed_but<AHEAD * (COPIES + 2)>();
+        else landed_but<AHEAD * (COPIES + 1)>();
+    };
 
     f32x4 acc[NI][NJ];
 #pragma unroll
@@ -106,39 +124,47 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
         for (int j = 0; j < NJ; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
     const int at = 16 * (g ^ (c & 7));   // place of piece g; piece g + 4 at the same ^ 64
-    copy(0, 0);
-    for (int kb = 0; kb < p.KB; ++kb) {
-        float s0[NJ], s1[NJ];
-        const float w0 = ws0[kb], w1 = ws1[kb];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const float v = xs[j][kb];
-            s0[j] = v * w0;
-            s1[j] = M == Mode::GateUp ? v * w1 : s0[j];
-        }
-        __builtin_amdgcn_s_waitcnt(wait_vm(0));
-        __builtin_amdgcn_s_barrier();
-        if (kb + 1 < p.KB) copy(kb + 1, (kb + 1) & 1);
-        const uint8_t *wl = lds + (kb & 1) * STAGE + (wn * NW + c) * kQ;
-        const uint8_t *xl = lds + (kb & 1) * STAGE + (BN + wt * TW + c) * kQ;
-        i32x8 b[NJ];
+    for (int i = 0; i < S - 1; ++i)
+        if (kb0 + i < kb1) copy(kb0 + i, i);
+    int slot = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+        landed(kb);
+        const int free = slot == 0 ? S - 1 : slot - 1;
+        if (kb + S - 1 < kb1) copy(kb + S - 1, free);
+        const uint8_t *stage = lds + slot * STAGE;
+        const uint8_t *wl = stage + (wn * NW + c) * kQ, *xl = stage + (BN + wt * TW + c) * kQ;
+        auto read = [&](const uint8_t *l, int i) {
+            l += 16 * kQ * i;
+            return pair(*(const u32x4 *)(l + at), *(const u32x4 *)(l + (at ^ 64)));
+        };
+        const float *sc = (const float *)(stage + CODES) + 128 * wave;
+        float s[NJ];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-            b[j] = pair(*(const u32x4 *)(xl + 16 * kQ * j + at), *(const u32x4 *)(xl + 16 * kQ * j + (at ^ 64)));
+        for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[64];
+        // weight rows are read one tile ahead of their products
+        i32x8 b[NJ], a = read(wl, 0);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) b[j] = read(xl, j);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const i32x8 a = pair(*(const u32x4 *)(wl + 16 * kQ * i + at), *(const u32x4 *)(wl + 16 * kQ * i + (at ^ 64)));
+            const i32x8 a2 = read(wl, i + 1 < NI ? i + 1 : i);
+            if (M == Mode::GateUp && i == NI / 2)   // on to the up rows
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[96];
             f32x4 v[NJ];
 #pragma unroll
             for (int j = 0; j < NJ; ++j) v[j] = mfma128<F32>(a, b[j]);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[i][j] += v[j] * (i < NI / 2 ? s0[j] : s1[j]);
+            for (int j = 0; j < NJ; ++j) acc[i][j] += v[j] * s[j];
+            a = a2;
         }
+        slot = slot + 1 == S ? 0 : slot + 1;
     }
 
     if constexpr (M == Mode::GateUp) {
         float *peak = (float *)lds;   // [WN][BT]
-        __builtin_amdgcn_s_barrier();   // the last step's reads are done
+        __syncthreads();   // the last step's reads are done
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             float m = 0.f;
@@ -185,16 +211,22 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 const int n = n0 + wn * NW + 16 * i + 4 * g;
-                store4<F32>(p, t, n, acc[i][j]);
+                if (splits > 1) {
+                    if (n < p.part_pitch)
+                        *(f32x4 *)(p.part + (split * (int64_t)p.T + t) * p.part_pitch + n) = acc[i][j];
+                } else {
+                    store4<F32>(p, t, n, acc[i][j]);
+                }
             }
         }
     }
 }
 
-template <Mode M, bool F32, int BN, int BT, int WN, int WT>
-hipError_t launch_tiled(const ProductArgs &p, int t_tiles, hipStream_t st) {
-    constexpr int bytes = 2 * (BN + BT) * kQ;
-    const auto kernel = tiled_kernel<M, F32, BN, BT, WN, WT>;
+template <Mode M, bool F32, int BN, int BT, int WN, int WT, int S>
+hipError_t launch_tiled(const ProductArgs &p, int t_tiles, int splits, hipStream_t st) {
+    constexpr int bytes = S * ((BN + BT) * kQ + 512 * WN * WT);
+    static_assert(bytes <= 160 * 1024);
+    const auto kernel = tiled_kernel<M, F32, BN, BT, WN, WT, S>;
     static std::atomic<uint64_t> ready{0};   // devices whose LDS limit is raised
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
@@ -205,8 +237,8 @@ hipError_t launch_tiled(const ProductArgs &p, int t_tiles, hipStream_t st) {
         if (dev < 64) ready.fetch_or(1ull << dev);
     }
     const int n_tiles = cdiv(p.N, M == Mode::GateUp ? BN / 2 : BN);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(n_tiles * t_tiles)), dim3(64 * WN * WT), bytes, st, p,
-                       n_tiles, t_tiles);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)n_tiles * t_tiles * splits)), dim3(64 * WN * WT),
+                       bytes, st, p, n_tiles, splits);
     return hipSuccess;
 }
 

@@ -8,7 +8,6 @@
 
 #include "echo_moe.h"
 #include "fp8.hpp"
-#include "fp8_stream.hpp"
 #include "fp8_tiled.hpp"
 #include "status.hpp"
 
@@ -150,40 +149,88 @@ void launch_route(const RouteArgs &a, hipStream_t st) {
 
 // ------------------------------------------------------------ the experts
 
-// Sorts the pairs by expert and cuts each expert's into tiles of `tile` rows:
-// counts, their prefix sums, then every pair to its place.  One workgroup.  The
-// order inside an expert is the order of the atomics, which no result hangs on:
-// a pair's row is computed alone and ends at the pair's own place.
-__global__ __launch_bounds__(1024) void sort_pairs_kernel(const int32_t *ids, int R, int E, int tile,
-                                                          int *num_tiles, Tile *tiles, int *order) {
-    __shared__ int count[kMaxExperts], first[kMaxExperts + 1], tfirst[kMaxExperts + 1];
+// The pairs in order of expert, each expert's cut into tiles of `tile` rows:
+// counts, their prefix sums, then every pair to its place.  Up to 64 workgroups
+// of 1,024 threads have `chunk` pairs each; more than one find the counts of all
+// chunks in `counts` [workgroup][E], from count_pairs_kernel.  The order inside an
+// expert is the order of the atomics, which no result hangs on: a pair's row is
+// computed alone and ends at the pair's own place.  37,120 pairs of 64 experts: 38
+// us in one workgroup.
+__global__ __launch_bounds__(1024) void count_pairs_kernel(const int32_t *ids, int R, int E, int chunk,
+                                                           int *counts) {
+    __shared__ int count[kMaxExperts];
     const int tid = threadIdx.x;
     if (tid < kMaxExperts) count[tid] = 0;
     __syncthreads();
-    for (int i = tid; i < R; i += 1024) {
+    const int end = min(R, (int)(blockIdx.x + 1) * chunk);
+    for (int i = blockIdx.x * chunk + tid; i < end; i += 1024) {
         const int e = ids[i];
         if (e >= 0 && e < E) atomicAdd(&count[e], 1);
     }
     __syncthreads();
-    if (tid == 0) {
-        int f = 0, tf = 0;
-        for (int e = 0; e < E; ++e) {
-            first[e] = f;
-            tfirst[e] = tf;
-            f += count[e];
-            tf += (count[e] + tile - 1) / tile;
+    if (tid < E) counts[blockIdx.x * E + tid] = count[tid];
+}
+
+__global__ __launch_bounds__(1024) void place_pairs_kernel(const int32_t *ids, int R, int E, int chunk,
+                                                           const int *counts, int tile, int *num_tiles,
+                                                           Tile *tiles, int *order) {
+    // of each expert: its pairs, then the next free place; the first place and tile
+    __shared__ int count[kMaxExperts], first[kMaxExperts], tfirst[kMaxExperts];
+    const int tid = threadIdx.x, me = blockIdx.x;
+    const int begin = me * chunk, end = min(R, begin + chunk);
+    int before = 0;   // pairs of expert tid in the chunks before this one
+    if (tid < kMaxExperts) {
+        int n = 0;
+        if (counts && tid < E)
+            for (int b = 0; b < (int)gridDim.x; ++b) {
+                const int c = counts[b * E + tid];
+                n += c;
+                before += b < me ? c : 0;
+            }
+        count[tid] = n;
+    }
+    __syncthreads();
+    if (!counts) {
+        for (int i = begin + tid; i < end; i += 1024) {
+            const int e = ids[i];
+            if (e >= 0 && e < E) atomicAdd(&count[e], 1);
         }
-        *num_tiles = tf;
+        __syncthreads();
+    }
+    if (tid < 64) {   // prefix sums, eight experts a lane
+        constexpr int PER = kMaxExperts / 64;
+        int n = 0, t = 0;
+        for (int i = 0; i < PER; ++i) {
+            const int c = count[PER * tid + i];
+            n += c;
+            t += (c + tile - 1) / tile;
+        }
+        int sn = n, st = t;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int an = __shfl_up(sn, o), at = __shfl_up(st, o);
+            if (tid >= o) sn += an, st += at;
+        }
+        if (tid == 63 && me == 0) *num_tiles = st;
+        sn -= n;
+        st -= t;
+        for (int i = 0; i < PER; ++i) {
+            const int c = count[PER * tid + i];
+            first[PER * tid + i] = sn;
+            tfirst[PER * tid + i] = st;
+            sn += c;
+            st += (c + tile - 1) / tile;
+        }
     }
     __syncthreads();
     if (tid < E) {
         const int n = count[tid], f = first[tid];
-        for (int i = 0; i * tile < n; ++i)
-            tiles[tfirst[tid] + i] = Tile{tid, f + i * tile, min(tile, n - i * tile), 0};
-        count[tid] = f;
+        if (me == 0)
+            for (int i = 0; i * tile < n; ++i)
+                tiles[tfirst[tid] + i] = Tile{tid, f + i * tile, min(tile, n - i * tile), 0};
+        count[tid] = f + before;
     }
     __syncthreads();
-    for (int i = tid; i < R; i += 1024) {
+    for (int i = begin + tid; i < end; i += 1024) {
         const int e = ids[i];
         if (e >= 0 && e < E) order[atomicAdd(&count[e], 1)] = i;
     }
@@ -232,7 +279,8 @@ namespace {
 
 struct Ws {
     int tile, max_tiles;   // rows of a tile, and the most tiles there can be
-    size_t num_tiles, tiles, order, hs, hc, y, total;
+    int chunk, chunks;     // pairs that a workgroup places, and workgroups
+    size_t num_tiles, counts, tiles, order, hs, hc, y, total;
 };
 
 int plan_ws(const echo_experts_t *x, int32_t T, int32_t top_k, Ws *w) {
@@ -250,15 +298,20 @@ int plan_ws(const echo_experts_t *x, int32_t T, int32_t top_k, Ws *w) {
     if (R > 1 << 24) return fail(ECHO_E_UNSUPPORTED, "%lld pairs of token and expert", (long long)R);
     const int E = x->num_experts;
     // tiles of as many pairs as experts get on average
-    const int64_t mean = R / E;
-    w->tile = mean > 128 ? 256 : mean > 32 ? 64 : mean > 16 ? 32 : 16;
+    // (measured either side, 64 experts of 2048 x 1024: 4 pairs an expert, 16 rows
+    // 87 us, 32 rows 87; 8: 101 and 90; 16: 32 rows 108, 64 rows 101; 64: 64 rows
+    // 133, 128 rows 160; 128: 199 and 193)
+    w->tile = R > 96 * (int64_t)E ? 128 : R > 12 * (int64_t)E ? 64 : R > 4 * (int64_t)E ? 32 : 16;
     w->max_tiles = (int)(R / w->tile + std::min<int64_t>(E, R));
     if ((int64_t)w->max_tiles * cdiv(x->hidden, 16) > INT32_MAX ||
         (int64_t)w->max_tiles * cdiv(x->intermediate, 16) > INT32_MAX)
         return fail(ECHO_E_UNSUPPORTED, "%lld pairs of token and expert", (long long)R);
     size_t o = 0;
     auto take = [&](size_t n) { const size_t at = o; o += (n + 255) / 256 * 256; return at; };
+    w->chunk = std::max(4096, cdiv(R, 64));
+    w->chunks = cdiv(R, w->chunk);
     w->num_tiles = take(4);
+    w->counts = take(4 * (size_t)E * w->chunks);
     w->tiles = take(sizeof(Tile) * w->max_tiles);
     w->order = take(4 * R);
     w->hs = take(4 * R * cdiv(x->intermediate, kQ));
@@ -273,24 +326,14 @@ int launched(const char *what) {
     return e == hipSuccess ? ECHO_OK : fail(ECHO_E_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-template <int TT>
-hipError_t stream_experts(const ProductArgs &gu, const ProductArgs &dn, int max_tiles, hipStream_t st) {
-    const int ib = cdiv(gu.N, kQ), hb = cdiv(dn.N, 16);
-    hipLaunchKernelGGL((stream_gate_up_kernel<TT>), dim3((unsigned)max_tiles * ib), dim3(512), 0, st,
-                       gu, ib);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((stream_kernel<Mode::Down, false, TT, 4>), dim3((unsigned)max_tiles * hb),
-                       dim3(256), 0, st, dn, hb);
-    return hipSuccess;
-}
-
-template <int BT, int WN, int WT>
-hipError_t tiled_experts(const ProductArgs &gu, const ProductArgs &dn, int max_tiles, hipStream_t st) {
-    hipError_t e = launch_tiled<Mode::GateUp, false, 256, BT, WN, WT>(gu, max_tiles, st);
+// The forms of both products: the gate and up rows of 128 columns, and rows of
+// the down matrix, by the tile's pairs.
+template <int BT, int GN, int GT, int GS, int BN, int DN, int DT, int DS>
+hipError_t run_experts(const ProductArgs &gu, const ProductArgs &dn, int max_tiles, hipStream_t st) {
+    hipError_t e = launch_tiled<Mode::GateUp, false, 256, BT, GN, GT, GS>(gu, max_tiles, 1, st);
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return launch_tiled<Mode::Down, false, 256, BT, WN, WT>(dn, max_tiles, st);
+    return launch_tiled<Mode::Down, false, BN, BT, DN, DT, DS>(dn, max_tiles, 1, st);
 }
 
 }  // namespace
@@ -374,9 +417,14 @@ int echo_moe_experts(const echo_experts_t *m, const void *x, const float *x_scal
     uint8_t *base = (uint8_t *)workspace;
     const int E = m->num_experts, H = m->hidden, I = m->intermediate, R = num_tokens * top_k;
     const int HB = cdiv(H, kQ), IB = cdiv(I, kQ);
-    hipLaunchKernelGGL(sort_pairs_kernel, dim3(1), dim3(1024), 0, st, ids, R, E, w.tile,
-                       (int *)(base + w.num_tiles), (Tile *)(base + w.tiles), (int *)(base + w.order));
-    if ((rc = launched("sorting of pairs"))) return rc;
+    int *counts = w.chunks > 1 ? (int *)(base + w.counts) : nullptr;
+    if (counts) {
+        hipLaunchKernelGGL(count_pairs_kernel, dim3(w.chunks), dim3(1024), 0, st, ids, R, E, w.chunk, counts);
+        if ((rc = launched("counting of pairs"))) return rc;
+    }
+    hipLaunchKernelGGL(place_pairs_kernel, dim3(w.chunks), dim3(1024), 0, st, ids, R, E, w.chunk, counts,
+                       w.tile, (int *)(base + w.num_tiles), (Tile *)(base + w.tiles), (int *)(base + w.order));
+    if ((rc = launched("placing of pairs"))) return rc;
 
     ProductArgs gu{};
     gu.x = (const uint8_t *)x;
@@ -408,10 +456,10 @@ int echo_moe_experts(const echo_experts_t *m, const void *x, const float *x_scal
     dn.y = base + w.y;
     dn.y_stride = H;
     dn.wide = true;   // H a multiple of 16, y the workspace's
-    const hipError_t e = w.tile == 256  ? tiled_experts<256, 2, 4>(gu, dn, w.max_tiles, st)
-                         : w.tile == 64 ? tiled_experts<64, 4, 1>(gu, dn, w.max_tiles, st)
-                         : w.tile == 32 ? stream_experts<2>(gu, dn, w.max_tiles, st)
-                                        : stream_experts<1>(gu, dn, w.max_tiles, st);
+    const hipError_t e = w.tile == 128  ? run_experts<128, 4, 2, 3, 256, 4, 2, 3>(gu, dn, w.max_tiles, st)
+                         : w.tile == 64 ? run_experts<64, 4, 2, 3, 128, 4, 1, 3>(gu, dn, w.max_tiles, st)
+                         : w.tile == 32 ? run_experts<32, 4, 1, 2, 128, 4, 1, 3>(gu, dn, w.max_tiles, st)
+                                        : run_experts<16, 8, 1, 2, 64, 4, 1, 4>(gu, dn, w.max_tiles, st);
     if (e != hipSuccess) return fail(ECHO_E_HIP, "experts' products: %s", hipGetErrorString(e));
     if ((rc = launched("experts' products"))) return rc;
     const int64_t n8 = (int64_t)num_tokens * H / 8;

@@ -38,82 +38,102 @@ def blocks(n: int) -> int:
     return -(-n // BLOCK)
 
 
-def _refuse(where: str, what: str):
+def refuse(where: str, what: str):
     raise echo.EchoError(echo.ECHO_E_INVALID, where, what)
 
 
-_dtypes = {}
+class _Types:
+    """Types that tensors may have (filled in at the first call: importing this
+    module does not import torch)."""
+    codes = f32 = bf16 = i32 = real = device = raw_stream = None
 
 
-def _kinds():
-    if not _dtypes:
+def types():
+    if _Types.real is None:
         import torch
-        _dtypes.update(codes=(torch.float8_e4m3fn, torch.uint8), f32=(torch.float32,),
-                       bf16=(torch.bfloat16,), i32=(torch.int32,),
-                       real=(torch.bfloat16, torch.float32))
-    return _dtypes
+        _Types.codes, _Types.f32 = (torch.float8_e4m3fn, torch.uint8), (torch.float32,)
+        _Types.bf16, _Types.i32 = (torch.bfloat16,), (torch.int32,)
+        # no GPU: a device that no tensor is on
+        _Types.device = torch.cuda.current_device if torch.cuda.is_available() else lambda: -2
+        _Types.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _Types.real = (torch.bfloat16, torch.float32)
+    return _Types
 
 
-def check(where: str, name: str, t, shape, kind: str, rows: bool = False) -> None:
-    """Refuses a tensor of another shape, type, device or layout: contiguous, or
-    with ``rows`` of contiguous rows any distance apart."""
-    if tuple(t.shape) != tuple(shape):
-        _refuse(where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    if t.dtype not in _kinds()[kind]:
-        _refuse(where, f"{name} has dtype {t.dtype}")
-    on_device(where, name, t)
-    if rows:
-        if t.numel() and (t.stride(-1) != 1 and t.shape[-1] > 1 or
-                          t.shape[0] > 1 and t.stride(0) < t.shape[-1]):
-            _refuse(where, f"the rows of {name} are not contiguous")
-    elif not t.is_contiguous():
-        _refuse(where, f"{name} is not contiguous")
+def _place(where: str, name: str, t, dev: int):
+    refuse(where, f"{name} is on {t.device}, " + (f"the current device is cuda:{dev}" if t.is_cuda
+                                                  else "not on a GPU"))
 
 
-def on_device(where: str, name: str, t) -> None:
-    import torch
-    if t.device.type != "cuda":
-        _refuse(where, f"{name} is on {t.device}, not on a GPU")
-    if t.device.index != torch.cuda.current_device():
-        _refuse(where, f"{name} is on {t.device}, the current device is "
-                       f"cuda:{torch.cuda.current_device()}")
+def address(where: str, name: str, t, shape, dtypes, dev: int) -> int:
+    """The address of a contiguous tensor of this shape, one of these types, on
+    the current device; refuses any other."""
+    if t.shape != shape:
+        refuse(where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.dtype not in dtypes:
+        refuse(where, f"{name} has dtype {t.dtype}")
+    if t.get_device() != dev:
+        _place(where, name, t, dev)
+    if not t.is_contiguous():
+        refuse(where, f"{name} is not contiguous")
+    return t.data_ptr()
 
 
-def row_stride(t) -> int:
-    return max(t.stride(0), t.shape[-1]) if t.shape[0] > 1 else max(1, t.shape[-1])
+def rows(where: str, name: str, t, shape, dtypes, dev: int):
+    """(address, elements from row to row) of a matrix whose rows are contiguous
+    and any distance apart."""
+    if t.shape != shape:
+        refuse(where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.dtype not in dtypes:
+        refuse(where, f"{name} has dtype {t.dtype}")
+    if t.get_device() != dev:
+        _place(where, name, t, dev)
+    n, m = shape
+    if t.is_contiguous():
+        return t.data_ptr(), max(m, 1)
+    s, one = t.stride()
+    if m > 1 and one != 1 or n > 1 and s < m:
+        refuse(where, f"the rows of {name} are not contiguous")
+    return t.data_ptr(), s if n > 1 else max(m, 1)
 
 
-def real_dtype(t) -> int:
-    import torch
-    return F32 if t.dtype is torch.float32 else BF16
-
-
-def _workspace(where: str, t):
-    """(pointer, bytes) of a workspace tensor or None."""
+def scratch(where: str, t, dev: int):
+    """(address, bytes) of a workspace tensor or None."""
     if t is None:
         return None, 0
-    on_device(where, "workspace", t)
+    if t.get_device() != dev:
+        _place(where, "workspace", t, dev)
     if not t.is_contiguous():
-        _refuse(where, "workspace is not contiguous")
-    return t.data_ptr(), t.numel() * t.element_size()
+        refuse(where, "workspace is not contiguous")
+    return t.data_ptr(), t.nbytes
+
+
+def stream_of(stream, dev: int) -> int:
+    return types().raw_stream(dev) if stream is None else stream.cuda_stream
 
 
 def quantize(x, codes, scales, block_rows: int = 1, stream=None) -> None:
     """Codes and scales of ``x`` [rows][cols] (rows any distance apart) or
     [batch][rows][cols], bf16 or fp32, in blocks of ``block_rows`` (1 or 128) x 128."""
-    where = "echo_fp8_quantize"
-    if x.dim() not in (2, 3):
-        _refuse(where, f"x has {x.dim()} axes")
-    if block_rows not in (1, BLOCK):
+    where, k = "echo_fp8_quantize", types()
+    dev = k.device()
+    shape = x.shape
+    if block_rows != 1 and block_rows != BLOCK:
         raise echo.EchoError(echo.ECHO_E_UNSUPPORTED, where, f"block_rows {block_rows}")
-    rows, cols = x.shape[-2:]
-    check(where, "x", x, x.shape, "real", rows=x.dim() == 2)
-    check(where, "codes", codes, x.shape, "codes")
-    check(where, "scales", scales, (*x.shape[:-2], -(-rows // block_rows), blocks(cols)), "f32")
-    batch = x.shape[0] if x.dim() == 3 else 1
-    echo._check(_lib().echo_fp8_quantize(
-        x.data_ptr(), real_dtype(x), row_stride(x) if x.dim() == 2 else cols, batch, rows, cols,
-        block_rows, codes.data_ptr(), scales.data_ptr(), echo._stream(stream)), where)
+    if len(shape) == 2:
+        batch, (n, cols), lead = 1, shape, ()
+        xp, stride = rows(where, "x", x, shape, k.real, dev)
+    elif len(shape) == 3:
+        batch, n, cols = shape
+        xp, stride, lead = address(where, "x", x, shape, k.real, dev), cols, (batch,)
+    else:
+        refuse(where, f"x has {x.dim()} axes")
+    cp = address(where, "codes", codes, shape, k.codes, dev)
+    sp = address(where, "scales", scales, (*lead, -(-n // block_rows), -(-cols // BLOCK)), k.f32, dev)
+    rc = _lib().echo_fp8_quantize(xp, F32 if x.dtype is k.f32[0] else BF16, stride, batch, n, cols,
+                                  block_rows, cp, sp, stream_of(stream, dev))
+    if rc:
+        echo._check(rc, where)
 
 
 def gemm_workspace_bytes(num_tokens: int, out_features: int, in_features: int) -> int:
@@ -129,21 +149,25 @@ def gemm(x, x_scale, w, w_scale, out, residual=None, workspace=None, stream=None
     """out [T][N] (bf16 or fp32, rows any distance apart) = x [T][K] times the
     transpose of w [N][K], plus ``residual`` (of out's type and strides; may be
     out itself).  ``workspace``: gemm_workspace_bytes() bytes, None where that is 0."""
-    where = "echo_fp8_gemm"
+    where, k = "echo_fp8_gemm", types()
+    dev = k.device()
     if x.dim() != 2 or w.dim() != 2:
-        _refuse(where, f"x has {x.dim()} axes, w {w.dim()}")
+        refuse(where, f"x has {x.dim()} axes, w {w.dim()}")
     (T, K), N = x.shape, w.shape[0]
-    check(where, "x", x, (T, K), "codes")
-    check(where, "x_scale", x_scale, (T, blocks(K)), "f32")
-    check(where, "w", w, (N, K), "codes")
-    check(where, "w_scale", w_scale, (blocks(N), blocks(K)), "f32")
-    check(where, "out", out, (T, N), "real", rows=True)
+    kb = -(-K // BLOCK)
+    xp = address(where, "x", x, (T, K), k.codes, dev)
+    xsp = address(where, "x_scale", x_scale, (T, kb), k.f32, dev)
+    wp = address(where, "w", w, (N, K), k.codes, dev)
+    wsp = address(where, "w_scale", w_scale, (-(-N // BLOCK), kb), k.f32, dev)
+    yp, stride = rows(where, "out", out, (T, N), k.real, dev)
+    rp = None
     if residual is not None:
-        check(where, "residual", residual, (T, N), "real", rows=True)
-        if residual.dtype is not out.dtype or row_stride(residual) != row_stride(out):
-            _refuse(where, "residual has not the type and strides of out")
-    wp, wb = _workspace(where, workspace)
-    echo._check(_lib().echo_fp8_gemm(
-        x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), T, N, K,
-        None if residual is None else residual.data_ptr(), out.data_ptr(), real_dtype(out),
-        row_stride(out), wp, wb, echo._stream(stream)), where)
+        rp, rs = rows(where, "residual", residual, (T, N), k.real, dev)
+        if residual.dtype is not out.dtype or rs != stride:
+            refuse(where, "residual has not the type and strides of out")
+    sp, sb = scratch(where, workspace, dev)
+    rc = _lib().echo_fp8_gemm(xp, xsp, wp, wsp, T, N, K, rp, yp,
+                              F32 if out.dtype is k.f32[0] else BF16, stride, sp, sb,
+                              stream_of(stream, dev))
+    if rc:
+        echo._check(rc, where)

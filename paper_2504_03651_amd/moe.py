@@ -54,22 +54,23 @@ class Router:
         self.num_experts, self.top_k = num_experts, top_k
         self.c = CRouter(num_experts, top_k, SCORES[score], num_groups, top_groups, group_top,
                          int(renormalize), scale)
+        self.ref = ctypes.byref(self.c)
 
 
 def route(router: Router, logits, ids, weights, bias=None, stream=None) -> None:
     """ids (int32) and weights (fp32) [T][top_k] of the experts chosen from
     ``logits`` [T][E] (bf16 or fp32, rows any distance apart); ``bias``: fp32 [E]."""
-    where = "echo_moe_route"
-    T = logits.shape[0]
-    fp8.check(where, "logits", logits, (T, router.num_experts), "real", rows=True)
-    fp8.check(where, "ids", ids, (T, router.top_k), "i32")
-    fp8.check(where, "weights", weights, (T, router.top_k), "f32")
-    if bias is not None:
-        fp8.check(where, "bias", bias, (router.num_experts,), "f32")
-    echo._check(_lib().echo_moe_route(
-        ctypes.byref(router.c), logits.data_ptr(), fp8.real_dtype(logits), fp8.row_stride(logits),
-        T, None if bias is None else bias.data_ptr(), ids.data_ptr(), weights.data_ptr(),
-        echo._stream(stream)), where)
+    where, k = "echo_moe_route", fp8.types()
+    dev = k.device()
+    T, E, n = logits.shape[0], router.num_experts, router.top_k
+    lp, stride = fp8.rows(where, "logits", logits, (T, E), k.real, dev)
+    ip = fp8.address(where, "ids", ids, (T, n), k.i32, dev)
+    wp = fp8.address(where, "weights", weights, (T, n), k.f32, dev)
+    bp = None if bias is None else fp8.address(where, "bias", bias, (E,), k.f32, dev)
+    rc = _lib().echo_moe_route(router.ref, lp, fp8.F32 if logits.dtype is k.f32[0] else fp8.BF16,
+                               stride, T, bp, ip, wp, fp8.stream_of(stream, dev))
+    if rc:
+        echo._check(rc, where)
 
 
 class Experts:
@@ -78,22 +79,25 @@ class Experts:
     [E][H][I] with scales [E][ceil(H/128)][ceil(I/128)]."""
 
     def __init__(self, w_gate_up, gate_up_scale, w_down, down_scale):
-        where = "Experts"
+        where, k = "Experts", fp8.types()
         if w_down.dim() != 3:
-            raise echo.EchoError(echo.ECHO_E_INVALID, where, f"w_down has {w_down.dim()} axes")
+            fp8.refuse(where, f"w_down has {w_down.dim()} axes")
         E, H, I = w_down.shape
         hb, ib = fp8.blocks(H), fp8.blocks(I)
-        fp8.check(where, "w_down", w_down, (E, H, I), "codes")
-        fp8.check(where, "w_gate_up", w_gate_up, (E, 2 * I, H), "codes")
-        fp8.check(where, "gate_up_scale", gate_up_scale, (E, 2, ib, hb), "f32")
-        fp8.check(where, "down_scale", down_scale, (E, hb, ib), "f32")
+        self.device = dev = w_down.get_device()
+        if dev < 0:
+            fp8.refuse(where, "w_down is not on a GPU")
         self.num_experts, self.hidden, self.intermediate = E, H, I
         self.t = (w_gate_up, gate_up_scale, w_down, down_scale)   # kept alive
-        self.c = CExperts(E, H, I, *[x.data_ptr() for x in self.t])
+        self.c = CExperts(E, H, I,
+                          fp8.address(where, "w_gate_up", w_gate_up, (E, 2 * I, H), k.codes, dev),
+                          fp8.address(where, "gate_up_scale", gate_up_scale, (E, 2, ib, hb), k.f32, dev),
+                          fp8.address(where, "w_down", w_down, (E, H, I), k.codes, dev),
+                          fp8.address(where, "down_scale", down_scale, (E, hb, ib), k.f32, dev))
+        self.ref = ctypes.byref(self.c)
 
     def workspace_bytes(self, num_tokens: int, top_k: int) -> int:
-        n = int(_lib().echo_moe_experts_workspace_bytes(ctypes.byref(self.c), int(num_tokens),
-                                                        int(top_k)))
+        n = int(_lib().echo_moe_experts_workspace_bytes(self.ref, int(num_tokens), int(top_k)))
         if n == 0 and echo.last_error():
             raise echo.EchoError(echo.ECHO_E_INVALID, "echo_moe_experts_workspace_bytes",
                                  echo.last_error())
@@ -104,19 +108,19 @@ def experts(ex: Experts, x, x_scale, ids, weights, out, workspace, residual=None
             stream=None) -> None:
     """out [T][H] bf16 = (residual +) the weighted sum of the outputs of the
     experts ``ids`` [T][top_k] for x (codes [T][H], scales [T][ceil(H/128)])."""
-    where = "echo_moe_experts"
-    T, H = x.shape
-    k = ids.shape[-1]
-    fp8.check(where, "x", x, (T, ex.hidden), "codes")
-    fp8.check(where, "x_scale", x_scale, (T, fp8.blocks(H)), "f32")
-    fp8.check(where, "ids", ids, (T, k), "i32")
-    fp8.check(where, "weights", weights, (T, k), "f32")
-    fp8.check(where, "out", out, (T, H), "bf16")
-    fp8.on_device(where, "w_down", ex.t[2])
-    if residual is not None:
-        fp8.check(where, "residual", residual, (T, H), "bf16")
-    wp, wb = fp8._workspace(where, workspace)
-    echo._check(_lib().echo_moe_experts(
-        ctypes.byref(ex.c), x.data_ptr(), x_scale.data_ptr(), T, k, ids.data_ptr(),
-        weights.data_ptr(), None if residual is None else residual.data_ptr(), out.data_ptr(),
-        wp, wb, echo._stream(stream)), where)
+    where, k = "echo_moe_experts", fp8.types()
+    dev = k.device()
+    if ex.device != dev:
+        fp8.refuse(where, f"the experts are on cuda:{ex.device}, the current device is cuda:{dev}")
+    T, H, n = x.shape[0], ex.hidden, ids.shape[-1]
+    xp = fp8.address(where, "x", x, (T, H), k.codes, dev)
+    xsp = fp8.address(where, "x_scale", x_scale, (T, -(-H // fp8.BLOCK)), k.f32, dev)
+    ip = fp8.address(where, "ids", ids, (T, n), k.i32, dev)
+    wp = fp8.address(where, "weights", weights, (T, n), k.f32, dev)
+    op = fp8.address(where, "out", out, (T, H), k.bf16, dev)
+    rp = None if residual is None else fp8.address(where, "residual", residual, (T, H), k.bf16, dev)
+    sp, sb = fp8.scratch(where, workspace, dev)
+    rc = _lib().echo_moe_experts(ex.ref, xp, xsp, T, n, ip, wp, rp, op, sp, sb,
+                                 fp8.stream_of(stream, dev))
+    if rc:
+        echo._check(rc, where)
