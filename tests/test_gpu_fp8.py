@@ -92,6 +92,27 @@ def test_quantize_fp32_edges():
             _same(_quantize(x[r:r + 1], torch.float32, block_rows), FO.quantize(x[r:r + 1], block_rows))
 
 
+def test_quantize_fp32_saturates_under_coarse_scales_and_keeps_infinities_apart():
+    """Scales of a few subnormal steps, whose quotients pass 448 and saturate, and
+    blocks with infinities and no NaN, beside ordinary blocks of the same rows."""
+    import torch
+    g = np.random.default_rng(4)
+    x = g.standard_normal((14, 1024)).astype(np.float32)
+    tiny = np.float32(2.0 ** -149)
+    for r, n in enumerate([448, 627, 660, 671, 672, 1000, 1119, 1120, 1343]):
+        x[r, 128:256] = 0
+        x[r, 128:132] = np.array([n, -n, n // 2, 1], np.float32) * tiny
+    x[9, 300], x[9, 301] = np.inf, -1.0
+    x[10, 1000] = -np.inf
+    x[11, 0:128] = np.inf
+    x[12] *= np.float32(2.0 ** 110)
+    x[13] *= np.float32(2.0 ** -110)
+    for block_rows in (1, 128):
+        _same(_quantize(x, torch.float32, block_rows), FO.quantize(x, block_rows))
+        for r in range(14):
+            _same(_quantize(x[r:r + 1], torch.float32, block_rows), FO.quantize(x[r:r + 1], block_rows))
+
+
 def _gemm(x, xs, w, ws, f32, residual=None, pad=0, stream=None):
     import torch
     from paper_2504_03651_amd import fp8
