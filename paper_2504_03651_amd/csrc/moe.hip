@@ -30,25 +30,68 @@ struct RouteArgs {
 };
 
 // x before y in falling order of (value, -index)
-__device__ __forceinline__ bool ahead(double xv, int xi, double yv, int yi) {
+template <typename V>
+__device__ __forceinline__ bool ahead(V xv, int xi, V yv, int yi) {
     return xv > yv || (xv == yv && xi < yi);
 }
 
-// One wave per token; lane l has experts l, l + 64, ...
+// LDS written by lanes of this wave is there for its other lanes
+__device__ __forceinline__ void wave_lds() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Groups by the sum of their best one or two of `value` (of all experts, in the
+// wave's LDS): the kept ones as bits group * lanes, in `keep`.  64 / (a power of
+// two of at least that many groups) lanes share a group.  exact: what is in LDS
+// decides; otherwise returns whether the last kept group is more than `apart`
+// times (1 + its magnitude) ahead of the first dropped one.
+template <typename V>
+__device__ __forceinline__ bool keep_groups(const RouteArgs &a, const V *value, int lanes, int lane,
+                                            bool exact, V apart, uint64_t &keep) {
+    const int per = a.E / a.groups, g = lane / lanes, sub = lane & (lanes - 1);
+    V b1 = -INFINITY, b2 = -INFINITY;
+    if (g < a.groups)
+        for (int j = sub; j < per; j += lanes) {
+            const V k = value[g * per + j];
+            b2 = k > b1 ? b1 : k > b2 ? k : b2;
+            b1 = k > b1 ? k : b1;
+        }
+    for (int o = 1; o < lanes; o <<= 1) {
+        const V c1 = __shfl_xor(b1, o), c2 = __shfl_xor(b2, o);
+        const V lo = b1 < c1 ? b1 : c1, hi = b2 < c2 ? c2 : b2;
+        b1 = b1 < c1 ? c1 : b1;
+        b2 = lo < hi ? hi : lo;
+    }
+    V v = a.group_top == 2 ? b1 + b2 : b1;
+    if (sizeof(V) == 8 && v > (V)DBL_MAX) v = (V)DBL_MAX;
+    int rank = 0;
+    for (int j = 0; j < a.groups; ++j) rank += ahead(__shfl(v, j * lanes), j, v, g);
+    keep = __ballot(sub == 0 && g < a.groups && rank < a.top_groups);
+    if (exact || a.top_groups == a.groups) return true;
+    const V last = __shfl(v, __ffsll((long long)__ballot(sub == 0 && g < a.groups && rank == a.top_groups - 1)) - 1);
+    const V next = __shfl(v, __ffsll((long long)__ballot(sub == 0 && g < a.groups && rank == a.top_groups)) - 1);
+    return last - next > apart * (1 + (last < 0 ? -last : last));
+}
+
+__device__ __forceinline__ int lanes_of_group(int groups) {
+    int l = 64;
+    while (64 / l < groups) l >>= 1;
+    return l;
+}
+
+// The definition, in 64 bits: what route_kernel takes where 32 do not decide.
+// id and weight of lane j: of the row's j-th expert.
 template <bool F32, bool SIGMOID, int PER>
-__global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
-    extern __shared__ double route_lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t t = (int64_t)blockIdx.x * 4 + wave;
-    const bool live = t < a.T;
-    double *row = route_lds + wave * (a.groups > 1 ? a.E + kMaxGroups : 0);
+__device__ __forceinline__ void route_row64(const RouteArgs &a, int64_t t, double *row, int lane,
+                                                      int &id, float &weight) {
     double score[PER], key[PER];
     double top = -DBL_MAX;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int e = lane + 64 * i;
         double z = -INFINITY;
-        if (live && e < a.E) {
+        if (e < a.E) {
             const int64_t at = t * a.stride + e;
             const float f = F32 ? ((const float *)a.logits)[at] : bf2f(((const uint16_t *)a.logits)[at]);
             if (f > -INFINITY) z = fmin((double)f, (double)FLT_MAX);   // not for NaN
@@ -81,37 +124,24 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
         }
     }
     if (a.groups > 1) {
-        const int per = a.E / a.groups;
+        const int per = a.E / a.groups, lanes = lanes_of_group(a.groups);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = lane + 64 * i;
             // a sum of two is of scores
             if (e < a.E) row[e] = a.group_top == 2 && !a.bias && key[i] > -INFINITY ? score[i] : key[i];
         }
-        __syncthreads();
-        double v = -INFINITY;
-        if (lane < a.groups) {
-            double b1 = -INFINITY, b2 = -INFINITY;
-            for (int j = 0; j < per; ++j) {
-                const double k = row[lane * per + j];
-                if (k > b1) b2 = b1, b1 = k;
-                else if (k > b2) b2 = k;
-            }
-            v = a.group_top == 2 ? fmin(b1 + b2, DBL_MAX) : b1;
-        }
-        int rank = 0;
-        for (int j = 0; j < a.groups; ++j) rank += ahead(__shfl(v, j), j, v, lane);
-        __syncthreads();
-        if (lane < a.groups) row[a.E + lane] = rank < a.top_groups ? 1.0 : 0.0;
-        __syncthreads();
+        wave_lds();
+        uint64_t keep;
+        keep_groups<double>(a, row, lanes, lane, true, 0.0, keep);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = lane + 64 * i;
-            if (e < a.E && row[a.E + e / per] == 0.0) key[i] = -INFINITY;
+            if (e < a.E && !(keep >> (e / per * lanes) & 1)) key[i] = -INFINITY;
         }
     }
     double mine = 0.0, sum = 0.0;   // lane j: the score of the row's j-th expert
-    int id = -1;
+    id = -1;
     for (int j = 0; j < a.top_k; ++j) {
         double v = -INFINITY, sc = 0.0;
         int at = 0x7FFFFFFF;
@@ -130,17 +160,177 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
         if (lane == j) id = at, mine = sc;
         sum += sc;
     }
-    if (live && lane < a.top_k) {
-        const double w = a.renormalize ? (sum > 0.0 ? mine / sum : 0.0) : mine;
+    const double w = a.renormalize ? (sum > 0.0 ? mine / sum : 0.0) : mine;
+    weight = (float)(w * (double)a.scale);
+}
+
+// fp32 as integers of the same order (no NaN; -0 and 0 made equal first)
+__device__ __forceinline__ int ordered(float x) {
+    const int b = __float_as_int(x);
+    return b ^ ((b >> 31) & 0x7FFFFFFF);
+}
+__device__ __forceinline__ float unordered(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
+
+// max over the wave: rotations in rows of 16 lanes, then swaps of rows and halves
+__device__ __forceinline__ int wave_max(int v) {
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, false));   // row_ror:8
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xF, 0xF, false));
+    const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = max((int)a[0], (int)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    return __builtin_amdgcn_readfirstlane(max((int)b[0], (int)b[1]));
+}
+
+// One wave per token; lane l has experts l, l + 64, ...  Without a bias the keys
+// are the logits, exact in fp32.  With one (or where groups go by sums of scores)
+// the keys come in fp32, off by less than off (1 + |key|): for a sigmoid s, s (1 -
+// s) 2^-23 from the exponential and 2^-24 s each from the sum and the quotient, with
+// the rounding of the key below 4 x 2^-24; for a softmax at most 20 roundings of a
+// score (its exponential's, the sum's over the lanes, the reciprocal's), below
+// 2^-19.  Where two neighbours among the chosen and the next, or the groups at
+// the border, are not further apart than that the row goes to route_row64.  The
+// chosen experts' scores are taken in 64 bits.  16,412 tokens of 256 experts with
+// groups and bias take 32 us (60 all in 64 bits), bound by instructions: nine
+// maxima over the wave and what finds them.
+
+template <bool F32, bool SIGMOID, int PER>
+__global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
+    extern __shared__ double route_lds[];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t = (int64_t)blockIdx.x * 4 + wave;
+    if (t >= a.T) return;
+    constexpr float off = SIGMOID ? 0x1p-22f : 0x1p-19f;
+    double *row = route_lds + wave * (a.groups > 1 ? a.E : 0);
+    float z[PER];
+    int key[PER];
+    const int none = ordered(-INFINITY);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = lane + 64 * i;
+        z[i] = -INFINITY;
+        if (e < a.E) {
+            const int64_t at = t * a.stride + e;
+            const float f = F32 ? ((const float *)a.logits)[at] : bf2f(((const uint16_t *)a.logits)[at]);
+            if (f > -INFINITY) z[i] = fminf(f, FLT_MAX) + 0.f;   // not for NaN; -0 becomes 0
+        }
+        key[i] = ordered(z[i]);
+    }
+    float top = 0.f;
+    if constexpr (!SIGMOID) {
+        int m = key[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) m = max(m, key[i]);
+        top = unordered(wave_max(m));
+    }
+    const bool sums = a.groups > 1 && a.group_top == 2 && !a.bias;   // groups by sums of scores
+    float sc[PER];
+    if (a.bias || sums) {
+        if constexpr (SIGMOID) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sc[i] = 1.f / (1.f + expf(-z[i]));
+        } else {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                sc[i] = z[i] == -INFINITY ? 0.f : expf(z[i] - top);
+                sum += sc[i];
+            }
+            for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+            const float r = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sc[i] *= r;
+        }
+        if (a.bias) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const float k = sc[i] + a.bias[min(lane + 64 * i, a.E - 1)];
+                key[i] = z[i] > -INFINITY && k > -INFINITY ? ordered(k) : none;   // not for NaN
+            }
+        }
+    }
+    bool sure = true;
+    if (a.groups > 1) {
+        float *value = (float *)row;
+        const int lanes = lanes_of_group(a.groups);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = lane + 64 * i;
+            if (e < a.E) value[e] = sums ? (z[i] > -INFINITY ? sc[i] : -INFINITY) : unordered(key[i]);
+        }
+        wave_lds();
+        uint64_t keep;
+        sure = keep_groups<float>(a, value, lanes, lane, !a.bias && !sums, 4 * off, keep);
+        const uint32_t per = a.E / a.groups, inv = ((1u << 20) + per - 1) / per;   // e / per, e < 512
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t e = lane + 64 * i;
+            if (!(keep >> ((e * inv >> 20) * lanes) & 1)) key[i] = none;
+        }
+    }
+    // lane j: the row's j-th expert and its logit
+    int id = -1;
+    float mine = -INFINITY, before = INFINITY;
+    for (int j = 0; j < a.top_k + (a.bias ? 1 : 0); ++j) {
+        int m = key[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) m = max(m, key[i]);
+        m = wave_max(m);
+        if (m <= none) break;
+        if (a.bias) {
+            const float v = unordered(m);
+            sure = sure && before - v > 2 * off * (1.f + fabsf(v));   // not for infinities
+            before = fminf(v, FLT_MAX);
+            if (v == INFINITY) sure = false;
+        }
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint64_t hit = __ballot(key[i] == m);
+            if (found || !hit) continue;
+            found = true;
+            const int l = __builtin_ctzll(hit);
+            const float zl = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(z[i]), l));
+            if (lane == l) key[i] = none;
+            if (lane == j) id = l + 64 * i, mine = zl;
+        }
+    }
+    if (a.bias && lane >= a.top_k) id = -1, mine = -INFINITY;   // the one looked at for its distance
+    float weight = 0.f;
+    if (!SIGMOID && __any(id >= 0 && mine - top < -690.f)) sure = false;   // scores near 64 bits' end
+    if (sure) {
+        double s = 0.0;
+        if constexpr (SIGMOID) {
+            if (id >= 0) s = 1.0 / (1.0 + exp(-(double)mine));
+        } else {
+            if (id >= 0) s = exp((double)mine - (double)top);
+        }
+        double sum = 1.0;
+        if (a.renormalize) {
+            sum = s;
+            for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+        } else if (!SIGMOID) {
+            sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sum += z[i] == -INFINITY ? 0.0 : exp((double)z[i] - (double)top);
+            for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+        }
+        weight = (float)((sum > 0.0 ? s / sum : 0.0) * (double)a.scale);
+    } else {
+        route_row64<F32, SIGMOID, PER>(a, t, row, lane, id, weight);
+    }
+    if (lane < a.top_k) {
         a.ids[t * a.top_k + lane] = id;
-        a.weights[t * a.top_k + lane] = (float)(w * (double)a.scale);
+        a.weights[t * a.top_k + lane] = weight;
     }
 }
 
 template <bool F32, bool SIGMOID>
 void launch_route(const RouteArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)cdiv(a.T, 4)), block(256);
-    const size_t lds = a.groups > 1 ? 4 * (a.E + kMaxGroups) * sizeof(double) : 0;
+    const size_t lds = a.groups > 1 ? 4 * a.E * sizeof(double) : 0;
     if (a.E <= 64) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 1>), grid, block, lds, st, a);
     else if (a.E <= 128) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 2>), grid, block, lds, st, a);
     else if (a.E <= 256) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 4>), grid, block, lds, st, a);

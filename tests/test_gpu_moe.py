@@ -68,6 +68,26 @@ def test_route_large_batch():
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("kw", [dict(top_k=6), dict(top_k=64),
+                                dict(top_k=6, num_groups=8, top_groups=3, group_top=2),
+                                dict(top_k=6, num_groups=8, top_groups=3)])
+def test_route_keys_closer_than_fp32_tells(score, kw):
+    """A bias that makes all keys of the first row equal but for its rounding to
+    fp32, so that 64 bits decide; the rows after it differ from the first in the
+    last bits of some logits, or altogether."""
+    E = 128
+    g = np.random.default_rng(6)
+    z = np.tile(g.standard_normal(E).astype(np.float32), (40, 1))
+    z[1:20] += (g.integers(-2, 3, (19, E)) * np.float32(2.0 ** -23)).astype(np.float32)
+    z[20:] = g.standard_normal((20, E)).astype(np.float32)
+    z64 = z[0].astype(np.float64)
+    s = np.exp(z64) / np.exp(z64).sum() if score == "softmax" else 1 / (1 + np.exp(-z64))
+    b = (0.75 - s).astype(np.float32)
+    kw = dict(kw, score=score, renormalize=True)
+    _same_route(_route(z, kw, b), FO.route(z, bias=b, **kw))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("groups", [1, 4])
 @pytest.mark.parametrize("group_top", [1, 2])
 @pytest.mark.parametrize("bias", [False, True])
