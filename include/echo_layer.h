@@ -38,6 +38,7 @@
 #include <stdint.h>
 
 #include "echo.h"
+#include "echo_moe.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -67,14 +68,47 @@ int echo_layer_forward(const echo_layer_t *layer, const echo_kv_pool_t *pool,
                        size_t workspace_bytes, void *host_workspace,
                        size_t host_workspace_bytes, void *stream);
 
-/* Per-stage GPU times of the calling thread's last echo_layer_forward while
- * echo_profile(1) is on: norms, qkv GEMM, RoPE, append, attention, o GEMM,
- * MLP GEMMs (gate_up + down) and the element-wise rest, in milliseconds. */
+/* Per-stage GPU times of the calling thread's last echo_layer_forward or
+ * echo_moe_layer_forward while echo_profile(1) is on: norms, qkv GEMM, RoPE,
+ * append, attention, o GEMM, MLP GEMMs (gate_up + down; or routing and experts)
+ * and the element-wise rest, in milliseconds. */
 typedef struct {
     float norm_ms, qkv_ms, rope_ms, append_ms, attention_ms, o_ms, mlp_ms, other_ms;
 } echo_layer_timing_t;
 
 int echo_layer_timing(echo_layer_timing_t *timing);
+
+/* The same layer with its weights in 8 bits and experts in the place of the MLP:
+ *
+ *   y   = RMSNorm(x) * attn_norm                        bf16
+ *   qkv = fp8(y) W_qkv^T                                bf16 (echo_fp8_quantize, _gemm)
+ *   q, k, v, RoPE, append, attention as above: o        fp32
+ *   h   = x + fp8(o) W_o^T                              bf16
+ *   y2  = RMSNorm(h) * mlp_norm                         bf16
+ *   ids, weights = route(y2 W_router^T)                 fp32 (hipBLASLt; echo_moe_route)
+ *   x'  = h + experts(fp8(y2), ids, weights)            bf16 (echo_moe_experts)
+ *
+ * w_qkv and w_o are e4m3 codes with scales of 128 x 128 blocks, w_router
+ * [num_experts][H] is bf16, router_bias fp32 [num_experts] or NULL.  router and
+ * experts agree in num_experts, experts.hidden is H, a multiple of 16. */
+typedef struct {
+    int32_t hidden;
+    int32_t num_q_heads, num_kv_heads, head_dim;
+    float rope_theta;
+    float rms_eps;
+    const void *attn_norm, *w_qkv, *w_o, *mlp_norm, *w_router;
+    const float *w_qkv_scale, *w_o_scale, *router_bias;
+    echo_router_t router;
+    echo_experts_t experts;
+} echo_moe_layer_t;
+
+/* As echo_layer_workspace_bytes and echo_layer_forward. */
+size_t echo_moe_layer_workspace_bytes(const echo_moe_layer_t *layer, const echo_kv_pool_t *pool,
+                                      const echo_batch_t *batch);
+int echo_moe_layer_forward(const echo_moe_layer_t *layer, const echo_kv_pool_t *pool,
+                           const echo_batch_t *batch, void *hidden, void *workspace,
+                           size_t workspace_bytes, void *host_workspace,
+                           size_t host_workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

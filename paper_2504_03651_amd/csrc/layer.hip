@@ -146,7 +146,7 @@ struct GemmPlan {
 
 struct Blas {
     hipblasLtHandle_t h = nullptr;
-    std::map<std::tuple<int64_t, int64_t, int64_t, bool>, GemmPlan> plans;
+    std::map<std::tuple<int64_t, int64_t, int64_t, bool, hipDataType>, GemmPlan> plans;
 };
 
 constexpr size_t kBlasWs = 32u << 20;
@@ -173,9 +173,9 @@ int get_blas(Blas **out) {
 }
 
 int gemm(Blas *bl, int64_t N, int64_t T, int64_t K, const void *W, const void *X,
-         const void *R, void *Y, void *ws, hipStream_t st) {
+         const void *R, void *Y, void *ws, hipStream_t st, hipDataType out = HIP_R_16BF) {
     const bool acc = R != nullptr;
-    auto key = std::make_tuple(N, T, K, acc);
+    auto key = std::make_tuple(N, T, K, acc, out);
     auto it = bl->plans.find(key);
     hipblasStatus_t s;
     if (it == bl->plans.end() && bl->plans.size() >= 256) {   // token counts vary per call
@@ -197,7 +197,7 @@ int gemm(Blas *bl, int64_t N, int64_t T, int64_t K, const void *W, const void *X
         hipblasLtMatmulDescSetAttribute(p.desc, HIPBLASLT_MATMUL_DESC_TRANSB, &opN, sizeof opN);
         if ((s = hipblasLtMatrixLayoutCreate(&p.a, HIP_R_16BF, K, N, K)) != HIPBLAS_STATUS_SUCCESS ||
             (s = hipblasLtMatrixLayoutCreate(&p.b, HIP_R_16BF, K, T, K)) != HIPBLAS_STATUS_SUCCESS ||
-            (s = hipblasLtMatrixLayoutCreate(&p.c, HIP_R_16BF, N, T, N)) != HIPBLAS_STATUS_SUCCESS)
+            (s = hipblasLtMatrixLayoutCreate(&p.c, out, N, T, N)) != HIPBLAS_STATUS_SUCCESS)
             return blas_fail(s, "hipblasLtMatrixLayoutCreate");
         hipblasLtMatmulPreference_t pref;
         if ((s = hipblasLtMatmulPreferenceCreate(&pref)) != HIPBLAS_STATUS_SUCCESS)
@@ -270,12 +270,98 @@ int plan_ws(const echo_layer_t *L, const echo_kv_pool_t *pool, const echo_batch_
     return ECHO_OK;
 }
 
+struct MoeWs {
+    size_t y, codes, scales, qkv, q, kn, vn, attn, attn_ws, h, logits, ids, weights, scratch, total;
+};
+
+// (the caller clears the error detail first)
+int plan_moe_ws(const echo_moe_layer_t *L, const echo_kv_pool_t *pool, const echo_batch_t *b,
+                MoeWs *w) {
+    if (!L || !pool || !b) return fail(ECHO_E_INVALID, "layer, pool or batch is NULL");
+    if (L->hidden <= 0 || L->num_q_heads <= 0 || L->num_kv_heads <= 0 ||
+        L->num_q_heads % L->num_kv_heads)
+        return fail(ECHO_E_INVALID, "layer shape (H %d, Hq %d, Hkv %d)", L->hidden, L->num_q_heads,
+                    L->num_kv_heads);
+    if (L->hidden % 16) return fail(ECHO_E_UNSUPPORTED, "hidden %d is not a multiple of 16", L->hidden);
+    if (L->head_dim != pool->head_dim || L->num_kv_heads != pool->num_kv_heads)
+        return fail(ECHO_E_INVALID, "layer heads (%d x %d) differ from the pool's (%d x %d)",
+                    L->num_kv_heads, L->head_dim, pool->num_kv_heads, pool->head_dim);
+    if (!L->attn_norm || !L->w_qkv || !L->w_qkv_scale || !L->w_o || !L->w_o_scale || !L->mlp_norm ||
+        !L->w_router)
+        return fail(ECHO_E_INVALID, "a layer weight or scale is NULL");
+    if (L->experts.hidden != L->hidden || L->experts.num_experts != L->router.num_experts)
+        return fail(ECHO_E_INVALID, "experts (H %d, %d experts) differ from the layer's (H %d, %d)",
+                    L->experts.hidden, L->experts.num_experts, L->hidden, L->router.num_experts);
+    // the router's, the experts' and the products' own checks, with no tokens
+    int rc = echo_moe_route(&L->router, nullptr, ECHO_F32, L->router.num_experts, 0, nullptr, nullptr,
+                            nullptr, nullptr);
+    if (!rc)
+        rc = echo_moe_experts(&L->experts, nullptr, nullptr, 0, L->router.top_k, nullptr, nullptr, nullptr,
+                              nullptr, nullptr, 0, nullptr);
+    if (!rc) rc = echo_validate(pool, b, 1);
+    if (rc) return rc;
+    const int64_t T = b->num_tokens, H = L->hidden, E = L->router.num_experts, k = L->router.top_k;
+    const int64_t qd = (int64_t)L->num_q_heads * L->head_dim;
+    const int64_t kd = (int64_t)L->num_kv_heads * L->head_dim;
+    if (qd + 2 * kd > INT32_MAX) return fail(ECHO_E_UNSUPPORTED, "%lld columns of qkv", (long long)(qd + 2 * kd));
+    const size_t attn_ws = echo_attn_workspace_bytes(pool, b, L->num_q_heads);
+    if (attn_ws == 0 && b->num_rows > 0) return ECHO_E_INVALID;   // detail already set
+    // one scratch for the products, the router's library product and the experts
+    size_t scratch = kBlasWs;
+    const int64_t shapes[2][2] = {{qd + 2 * kd, H}, {H, qd}};
+    for (const auto &s : shapes) {
+        const size_t n = echo_fp8_gemm_workspace_bytes((int32_t)T, (int32_t)s[0], (int32_t)s[1]);
+        if (n == 0 && *echo_last_error()) return ECHO_E_UNSUPPORTED;   // detail already set
+        scratch = std::max(scratch, n);
+    }
+    const size_t ex = echo_moe_experts_workspace_bytes(&L->experts, (int32_t)T, (int32_t)k);
+    if (ex == 0 && T > 0) return ECHO_E_UNSUPPORTED;   // detail already set
+    scratch = std::max(scratch, ex);
+    const int64_t wide = std::max(H, qd);
+    size_t o = 0;
+    auto take = [&](size_t n) { const size_t at = o; o += up256(n); return at; };
+    w->y = take(T * H * 2);
+    w->codes = take(T * wide);
+    w->scales = take(T * ((wide + 127) / 128) * 4);
+    w->qkv = take(T * (qd + 2 * kd) * 2);
+    w->q = take(T * qd * 2);
+    w->kn = take(T * kd * 2);
+    w->vn = take(T * kd * 2);
+    w->attn = take(T * qd * 4);
+    w->attn_ws = take(std::max<size_t>(attn_ws, 256));
+    w->h = take(T * H * 2);
+    w->logits = take(T * E * 4);
+    w->ids = take(T * k * 4);
+    w->weights = take(T * k * 4);
+    w->scratch = take(scratch);
+    w->total = o;
+    return ECHO_OK;
+}
+
 struct LayerProfile {
     int device = -1;
     hipEvent_t ev[12] = {};
     bool valid = false;
 };
 thread_local LayerProfile g_lprof;
+
+// *ev: the calling thread's stage events on this device while profiling is on
+int stage_events(hipEvent_t **ev) {
+    *ev = nullptr;
+    if (!echo::profile_enabled()) return ECHO_OK;
+    int dev = 0;
+    (void)hipGetDevice(&dev);
+    if (g_lprof.device != dev) {
+        for (hipEvent_t &e : g_lprof.ev)
+            if (e) (void)hipEventDestroy(e), e = nullptr;
+        g_lprof.device = dev;
+    }
+    for (hipEvent_t &e : g_lprof.ev)
+        if (!e && hipEventCreate(&e) != hipSuccess) return fail(ECHO_E_HIP, "hipEventCreate");
+    *ev = g_lprof.ev;
+    g_lprof.valid = false;
+    return ECHO_OK;
+}
 
 }  // namespace
 
@@ -319,19 +405,7 @@ int echo_layer_forward(const echo_layer_t *L, const echo_kv_pool_t *pool,
 
     // stage events (profiling only): 0 start, then after each stage
     hipEvent_t *ev = nullptr;
-    if (echo::profile_enabled()) {
-        int dev = 0;
-        (void)hipGetDevice(&dev);
-        if (g_lprof.device != dev) {
-            for (hipEvent_t &e : g_lprof.ev)
-                if (e) (void)hipEventDestroy(e), e = nullptr;
-            g_lprof.device = dev;
-        }
-        for (hipEvent_t &e : g_lprof.ev)
-            if (!e && hipEventCreate(&e) != hipSuccess) return fail(ECHO_E_HIP, "hipEventCreate");
-        ev = g_lprof.ev;
-        g_lprof.valid = false;
-    }
+    if ((rc = stage_events(&ev))) return rc;
     auto mark = [&](int i) {
         if (ev) (void)hipEventRecord(ev[i], st);
     };
@@ -377,6 +451,102 @@ int echo_layer_forward(const echo_layer_t *L, const echo_kv_pool_t *pool,
     if ((rc = check("silu_mul"))) return rc;
     mark(10);
     if ((rc = gemm(bl, H, T, I, L->w_down, act, h, x, bws, st))) return rc;
+    mark(11);
+    if (ev) g_lprof.valid = true;
+    return ECHO_OK;
+}
+
+size_t echo_moe_layer_workspace_bytes(const echo_moe_layer_t *layer, const echo_kv_pool_t *pool,
+                                      const echo_batch_t *batch) {
+    echo::clear_error();
+    MoeWs w;
+    if (plan_moe_ws(layer, pool, batch, &w)) return 0;
+    return w.total;
+}
+
+int echo_moe_layer_forward(const echo_moe_layer_t *L, const echo_kv_pool_t *pool,
+                           const echo_batch_t *batch, void *hidden, void *workspace,
+                           size_t workspace_bytes, void *host_workspace,
+                           size_t host_workspace_bytes, void *stream) {
+    echo::clear_error();
+    MoeWs w;
+    int rc = plan_moe_ws(L, pool, batch, &w);
+    if (rc) return rc;
+    if (batch->num_rows == 0) return ECHO_OK;
+    if (!hidden) return fail(ECHO_E_INVALID, "hidden is NULL");
+    if (((uintptr_t)hidden | (uintptr_t)L->attn_norm | (uintptr_t)L->mlp_norm | (uintptr_t)L->w_qkv |
+         (uintptr_t)L->w_o | (uintptr_t)L->w_router) & 15u)
+        return fail(ECHO_E_INVALID, "hidden and the layer's weights must be 16-byte aligned");
+    if (((uintptr_t)L->w_qkv_scale | (uintptr_t)L->w_o_scale | (uintptr_t)L->router_bias) & 3u)
+        return fail(ECHO_E_INVALID, "scales and router_bias must be 4-byte aligned");
+    if (!workspace || workspace_bytes < w.total || ((uintptr_t)workspace & 255u))
+        return fail(ECHO_E_WORKSPACE, "workspace of %zu bytes (need %zu, 256-byte aligned)",
+                    workspace_bytes, w.total);
+    Blas *bl = nullptr;
+    if ((rc = get_blas(&bl))) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    uint8_t *base = (uint8_t *)workspace;
+    uint16_t *x = (uint16_t *)hidden, *y = (uint16_t *)(base + w.y), *qkv = (uint16_t *)(base + w.qkv);
+    uint16_t *q = (uint16_t *)(base + w.q), *kn = (uint16_t *)(base + w.kn), *vn = (uint16_t *)(base + w.vn);
+    uint16_t *h = (uint16_t *)(base + w.h);
+    float *attn = (float *)(base + w.attn), *scales = (float *)(base + w.scales);
+    float *logits = (float *)(base + w.logits), *weights = (float *)(base + w.weights);
+    int32_t *ids = (int32_t *)(base + w.ids);
+    void *codes = base + w.codes, *scratch = base + w.scratch;
+    const size_t scratch_bytes = w.total - w.scratch;
+    const int T = batch->num_tokens, H = L->hidden, E = L->router.num_experts;
+    const int Hq = L->num_q_heads, Hkv = L->num_kv_heads, D = L->head_dim;
+    const int qd = Hq * D, width = (Hq + 2 * Hkv) * D;
+
+    hipEvent_t *ev = nullptr;
+    if ((rc = stage_events(&ev))) return rc;
+    auto mark = [&](int i) {
+        if (ev) (void)hipEventRecord(ev[i], st);
+    };
+    auto check = [&](const char *what) -> int {
+        hipError_t e = hipGetLastError();
+        return e == hipSuccess ? ECHO_OK : fail(ECHO_E_HIP, "%s: %s", what, hipGetErrorString(e));
+    };
+    mark(0);
+    hipLaunchKernelGGL(rmsnorm_kernel, dim3(T), dim3(256), 0, st, x, (const uint16_t *)L->attn_norm, y, H,
+                       L->rms_eps);
+    if ((rc = check("rmsnorm"))) return rc;
+    mark(1);
+    if ((rc = echo_fp8_quantize(y, ECHO_BF16, H, 1, T, H, 1, codes, scales, stream))) return rc;
+    if ((rc = echo_fp8_gemm(codes, scales, L->w_qkv, L->w_qkv_scale, T, width, H, nullptr, qkv, ECHO_BF16,
+                            width, scratch, scratch_bytes, stream)))
+        return rc;
+    mark(2);
+    hipLaunchKernelGGL(rope_split_kernel, dim3(T), dim3(256), 0, st, qkv, batch->q_start, batch->seq_lens,
+                       batch->num_rows, Hq, Hkv, D, std::log2((double)L->rope_theta), q, kn, vn);
+    if ((rc = check("rope"))) return rc;
+    mark(3);
+    if ((rc = echo_kv_append(pool, batch, kn, vn, stream))) return rc;
+    mark(4);
+    if ((rc = echo_attn_mixed(pool, batch, q, Hq, (float)(1.0 / std::sqrt((double)D)), attn,
+                              base + w.attn_ws, w.h - w.attn_ws, host_workspace, host_workspace_bytes,
+                              stream)))
+        return rc;
+    mark(5);
+    if ((rc = echo_fp8_quantize(attn, ECHO_F32, qd, 1, T, qd, 1, codes, scales, stream))) return rc;
+    mark(6);
+    if ((rc = echo_fp8_gemm(codes, scales, L->w_o, L->w_o_scale, T, H, qd, x, h, ECHO_BF16, H, scratch,
+                            scratch_bytes, stream)))
+        return rc;
+    mark(7);
+    hipLaunchKernelGGL(rmsnorm_kernel, dim3(T), dim3(256), 0, st, h, (const uint16_t *)L->mlp_norm, y, H,
+                       L->rms_eps);
+    if ((rc = check("rmsnorm"))) return rc;
+    mark(8);
+    if ((rc = gemm(bl, E, T, H, L->w_router, y, nullptr, logits, scratch, st, HIP_R_32F))) return rc;
+    if ((rc = echo_moe_route(&L->router, logits, ECHO_F32, E, T, L->router_bias, ids, weights, stream)))
+        return rc;
+    mark(9);
+    if ((rc = echo_fp8_quantize(y, ECHO_BF16, H, 1, T, H, 1, codes, scales, stream))) return rc;
+    mark(10);
+    if ((rc = echo_moe_experts(&L->experts, codes, scales, T, L->router.top_k, ids, weights, h, x, scratch,
+                               scratch_bytes, stream)))
+        return rc;
     mark(11);
     if (ev) g_lprof.valid = true;
     return ECHO_OK;

@@ -474,6 +474,49 @@ def layer_weights(seed: int, hidden: int, num_q_heads: int, num_kv_heads: int, h
         _scaled_bf16(seed, 45, H * I, 1.0 / math.sqrt(I)).reshape(H, I))
 
 
+@dataclass
+class MoELayerWeights:
+    """Weights of the layer with experts, bf16 bits before they are quantised."""
+    hidden: int
+    num_q_heads: int
+    num_kv_heads: int
+    head_dim: int
+    intermediate: int         # of each expert
+    num_experts: int
+    rope_theta: float
+    rms_eps: float
+    attn_norm: np.ndarray     # [H]
+    w_qkv: np.ndarray         # [(Hq + 2 Hkv) D][H]
+    w_o: np.ndarray           # [H][Hq D]
+    mlp_norm: np.ndarray      # [H]
+    w_router: np.ndarray      # [E][H]
+    router_bias: np.ndarray   # [E] fp32
+    w_gate_up: np.ndarray     # [E][2 I][H] (gate rows, then up rows)
+    w_down: np.ndarray        # [E][H][I]
+
+
+def moe_layer_weights(seed: int, hidden: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
+                      intermediate: int, num_experts: int, router_scale: float = 2.0,
+                      rope_theta: float = 500000.0, rms_eps: float = 1e-5) -> MoELayerWeights:
+    """Random weights: linear layers N(0, 1/fan_in), the router's times
+    ``router_scale`` (logits of that spread), norms 1 + N(0, 0.1^2), biases
+    N(0, 0.1^2)."""
+    H, I, E = hidden, intermediate, num_experts
+    qkv = (num_q_heads + 2 * num_kv_heads) * head_dim
+    qd = num_q_heads * head_dim
+    g = np.random.Generator(np.random.PCG64(np.random.SeedSequence([seed, 55])))
+    return MoELayerWeights(
+        hidden, num_q_heads, num_kv_heads, head_dim, intermediate, num_experts, rope_theta, rms_eps,
+        _scaled_bf16(seed, 50, H, 0.1, 1.0),
+        _scaled_bf16(seed, 51, qkv * H, 1.0 / math.sqrt(H)).reshape(qkv, H),
+        _scaled_bf16(seed, 52, H * qd, 1.0 / math.sqrt(qd)).reshape(H, qd),
+        _scaled_bf16(seed, 53, H, 0.1, 1.0),
+        _scaled_bf16(seed, 54, E * H, router_scale / math.sqrt(H)).reshape(E, H),
+        (0.1 * g.standard_normal(E)).astype(np.float32),
+        _scaled_bf16(seed, 56, E * 2 * I * H, 1.0 / math.sqrt(H)).reshape(E, 2 * I, H),
+        _scaled_bf16(seed, 57, E * H * I, 1.0 / math.sqrt(I)).reshape(E, H, I))
+
+
 def layer_hidden(seed: int, num_tokens: int, hidden: int) -> np.ndarray:
     """The layer's input activations [T][H]: N(0,1) bf16 bits."""
     return _scaled_bf16(seed, 46, num_tokens * hidden, 1.0).reshape(num_tokens, hidden)

@@ -185,3 +185,44 @@ def test_binding_refuses_host_tensors_and_wrong_layouts():
         moe.route(moe.Router(64, 4), x, scales, scales)
     with pytest.raises(echo.EchoError, match="score"):
         moe.Router(64, 4, score="tanh")
+
+
+def _moe_layer(**change):
+    from paper_2504_03651_amd import layer
+    v = dict(hidden=256, num_q_heads=4, num_kv_heads=4, head_dim=64, rope_theta=1e4, rms_eps=1e-5,
+             attn_norm=P, w_qkv=P, w_o=P, mlp_norm=P, w_router=P, w_qkv_scale=P, w_o_scale=P,
+             router_bias=None, router=moe.CRouter(8, 2, 0, 1, 1, 1, 0, 1.0),
+             experts=moe.CExperts(*EXPERTS.values()))
+    return layer, layer.CMoELayer(*{**v, **change}.values())
+
+
+@pytest.mark.parametrize("change, code, what", [
+    (dict(hidden=0), INV, "shape"), (dict(hidden=264), UNS, "multiple of 16"),
+    (dict(num_q_heads=6), INV, "shape"), (dict(head_dim=128), INV, "differ from the pool"),
+    (dict(w_qkv=None), INV, "NULL"), (dict(w_o_scale=None), INV, "NULL"), (dict(w_router=None), INV, "NULL"),
+    (dict(router=moe.CRouter(4, 2, 0, 1, 1, 1, 0, 1.0)), INV, "experts"),
+    (dict(router=moe.CRouter(8, 9, 0, 1, 1, 1, 0, 1.0)), INV, "top_k"),
+    (dict(hidden=272), INV, "experts"),
+    (dict(experts=moe.CExperts(*{**EXPERTS, "w_down": None}.values())), INV, "NULL"),
+    (dict(attn_norm=at(8)), INV, "16-byte"), (dict(w_o_scale=at(2)), INV, "4-byte"),
+])
+def test_moe_layer_refusals(change, code, what):
+    from paper_2504_03651_amd import workload as W
+    layer, c = _moe_layer(**change)
+    cp, cb, keep = echo.host_structs(W.config1())
+    rc = layer._lib().echo_moe_layer_forward(ctypes.byref(c), ctypes.byref(cp), ctypes.byref(cb), P, P, 1 << 40,
+                                             None, 0, None)
+    assert rc == code and what in echo.last_error(), echo.last_error()
+
+
+def test_moe_layer_workspace():
+    from paper_2504_03651_amd import workload as W
+    layer, c = _moe_layer()
+    cp, cb, keep = echo.host_structs(W.config1())
+    args = (ctypes.byref(c), ctypes.byref(cp), ctypes.byref(cb))
+    n = layer._lib().echo_moe_layer_workspace_bytes(*args)
+    assert n > 0
+    for hidden, ws, nb, code in [(None, P, n, INV), (P, None, n, WSP), (P, P, n - 1, WSP), (P, at(128), n, WSP)]:
+        assert layer._lib().echo_moe_layer_forward(*args, hidden, ws, nb, None, 0, None) == code
+    cb.num_tokens += 1
+    assert layer._lib().echo_moe_layer_workspace_bytes(*args) == 0 and echo.last_error()
