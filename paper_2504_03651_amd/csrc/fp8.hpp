@@ -108,6 +108,7 @@ struct ProductArgs {
     void *y;
     int64_t y_stride;
     bool wide;             // see store4
+    bool pieces;           // wide, with rows of y at 16-byte steps and N a multiple of 8
     float *part;           // [splits][T][part_pitch], for products over ranges of K
     int part_pitch;
     // GateUp
@@ -119,6 +120,12 @@ struct ProductArgs {
     const int *order;      // pair of each place
     int top_k;
 };
+
+// LDS written by lanes of this wave is there for its other lanes
+__device__ __forceinline__ void wave_lds() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 
 // y of a lane's four columns n .. n + 3 of row t, the residual added; p.wide:
 // N and y_stride multiples of 4, y and residual aligned to four values

@@ -18,6 +18,117 @@ __device__ __forceinline__ void landed_but() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// What a tile's workgroup does with its sums.  Results of 16 bits and codes go
+// through LDS, so that a store instruction writes whole pieces of rows: the tile
+// has them by columns, four values of a row a lane.
+// Uses at most BN * BT * 2 bytes of LDS (GateUp: BT * (128 + 4 WN)).
+template <Mode M, bool F32, int BN, int BT, int WN, int WT>
+__device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
+                                       f32x4 (&acc)[BN / WN / 16][BT / WT / 16], int n_tiles, int nb,
+                                       int n0, int row0, int rows, int splits, int split) {
+    constexpr int NW = BN / WN, TW = BT / WT, NI = NW / 16, NJ = TW / 16;
+    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wn = wave % WN, wt = wave / WN;
+    if constexpr (M == Mode::GateUp) {
+        float *peak = (float *)(lds + BT * kQ);   // [WN][BT]
+        __syncthreads();   // the last step's reads are done
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            float m = 0.f;
+#pragma unroll
+            for (int i = 0; i < NI / 2; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float a = acc[i][j][r];
+                    const float h = n0 + wn * (NW / 2) + 16 * i < p.N
+                                        ? a / (1.f + expf(-a)) * acc[NI / 2 + i][j][r] : 0.f;
+                    acc[i][j][r] = h;
+                    m = fmaxf(m, fabsf(h));   // a NaN keeps out
+                }
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            if (g == 0) peak[wn * BT + wt * TW + 16 * j + c] = m;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const int r = wt * TW + 16 * j + c;
+            float m = peak[r];
+#pragma unroll
+            for (int v = 1; v < WN; ++v) m = fmaxf(m, peak[v * BT + r]);
+            const float s = scale_of(m);
+            if (wn == 0 && g == 0 && r < rows) p.hs[(int64_t)(row0 + r) * n_tiles + nb] = s;
+            // h / s by the reciprocal, both times 2^64 where that could overflow
+            const float f = s < 0x1p-64f ? 0x1p64f : 1.f, inv = 1.f / (s * f);
+#pragma unroll
+            for (int i = 0; i < NI / 2; ++i) {
+                const f32x4 h = acc[i][j] * f * inv;
+                // 16-byte piece q of row r at place q ^ (r & 7)
+                const int at = wn * (NW / 2) + 16 * i + 4 * g;
+                *(uint32_t *)(lds + r * kQ + 16 * ((at >> 4) ^ (r & 7)) + (at & 15)) =
+                    e4m3x2(h[0], h[1]) | (e4m3x2(h[2], h[3]) << 16);
+            }
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < 8 * rows; e += 64 * WN * WT) {
+            const int r = e >> 3, q = e & 7;
+            if (n0 + 16 * q < p.N)   // N a multiple of 16
+                *(u32x4 *)(p.hc + (int64_t)(row0 + r) * p.N + n0 + 16 * q) =
+                    *(const u32x4 *)(lds + r * kQ + 16 * (q ^ (r & 7)));
+        }
+    } else if (splits > 1 || F32 || !p.pieces) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const int r = wt * TW + 16 * j + c;
+            if (r >= rows) continue;
+            const int64_t t = M == Mode::Down ? p.order[row0 + r] : row0 + r;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int n = n0 + wn * NW + 16 * i + 4 * g;
+                if (splits > 1) {
+                    if (n < p.part_pitch)
+                        *(f32x4 *)(p.part + (split * (int64_t)p.T + t) * p.part_pitch + n) = acc[i][j];
+                } else {
+                    store4<F32>(p, t, n, acc[i][j]);
+                }
+            }
+        }
+    } else {
+        constexpr int Q = NW / 8;   // 16-byte pieces of a row of this wave
+        uint8_t *mine = lds + wave * (NW * TW * 2);
+        __syncthreads();   // the last step's reads are done
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const int r = 16 * j + c;
+            const bool live = wt * TW + r < rows;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                f32x4 v = acc[i][j];
+                const int n = 16 * i + 4 * g;
+                if (M == Mode::Plain && p.residual && live && n0 + wn * NW + n < p.N) {
+                    const u32x2 q = *(const u32x2 *)((const uint16_t *)p.residual +
+                                                     (row0 + wt * TW + r) * p.y_stride + n0 + wn * NW + n);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) v[2 * e] += bf2f(q[e] & 0xFFFFu), v[2 * e + 1] += bf2f(q[e] >> 16);
+                }
+                *(u32x2 *)(mine + (r * Q + ((n >> 3) ^ (r & (Q - 1)))) * 16 + (n & 4) * 2) =
+                    (u32x2){f2bf(v[0]) | (f2bf(v[1]) << 16), f2bf(v[2]) | (f2bf(v[3]) << 16)};
+            }
+        }
+        wave_lds();
+        const int q = lane % Q, n = n0 + wn * NW + 8 * q;
+#pragma unroll
+        for (int r0 = 0; r0 < TW; r0 += 64 / Q) {
+            const int r = r0 + lane / Q, row = wt * TW + r;
+            if (row >= rows || n >= p.N) continue;
+            const int64_t t = M == Mode::Down ? p.order[row0 + row] : row0 + row;
+            *(u32x4 *)((uint16_t *)p.y + t * p.y_stride + n) =
+                *(const u32x4 *)(mine + (r * Q + (q ^ (r & (Q - 1)))) * 16);
+        }
+    }
+}
+
 // One workgroup of WN x WT waves: BN weight rows (GateUp: BN / 2 gate rows and
 // the up rows of the same columns) by BT tokens, K in steps of 128 through a ring
 // of S LDS stages that are filled straight from memory, S - 1 steps ahead.  A
@@ -162,72 +273,13 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
         slot = slot + 1 == S ? 0 : slot + 1;
     }
 
-    if constexpr (M == Mode::GateUp) {
-        float *peak = (float *)lds;   // [WN][BT]
-        __syncthreads();   // the last step's reads are done
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            float m = 0.f;
-#pragma unroll
-            for (int i = 0; i < NI / 2; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float a = acc[i][j][r];
-                    const float h = n0 + wn * (NW / 2) + 16 * i < p.N
-                                        ? a / (1.f + expf(-a)) * acc[NI / 2 + i][j][r] : 0.f;
-                    acc[i][j][r] = h;
-                    m = fmaxf(m, fabsf(h));   // a NaN keeps out
-                }
-            m = fmaxf(m, __shfl_xor(m, 16));
-            m = fmaxf(m, __shfl_xor(m, 32));
-            if (g == 0) peak[wn * BT + wt * TW + 16 * j + c] = m;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int r = wt * TW + 16 * j + c;
-            if (r >= rows) continue;
-            float m = peak[r];
-#pragma unroll
-            for (int v = 1; v < WN; ++v) m = fmaxf(m, peak[v * BT + r]);
-            const float s = scale_of(m);
-            const int64_t row = row0 + r;
-            if (wn == 0 && g == 0) p.hs[row * n_tiles + nb] = s;
-#pragma unroll
-            for (int i = 0; i < NI / 2; ++i) {
-                const int n = n0 + wn * (NW / 2) + 16 * i + 4 * g;
-                const f32x4 h = acc[i][j];
-                if (n < p.N)   // N a multiple of 16
-                    *(uint32_t *)(p.hc + row * p.N + n) =
-                        e4m3x2(h[0] / s, h[1] / s) | (e4m3x2(h[2] / s, h[3] / s) << 16);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int r = wt * TW + 16 * j + c;
-            if (r >= rows) continue;
-            const int64_t t = M == Mode::Down ? p.order[row0 + r] : row0 + r;
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int n = n0 + wn * NW + 16 * i + 4 * g;
-                if (splits > 1) {
-                    if (n < p.part_pitch)
-                        *(f32x4 *)(p.part + (split * (int64_t)p.T + t) * p.part_pitch + n) = acc[i][j];
-                } else {
-                    store4<F32>(p, t, n, acc[i][j]);
-                }
-            }
-        }
-    }
+    finish<M, F32, BN, BT, WN, WT>(p, lds, acc, n_tiles, nb, n0, row0, rows, splits, split);
 }
 
-template <Mode M, bool F32, int BN, int BT, int WN, int WT, int S>
-hipError_t launch_tiled(const ProductArgs &p, int t_tiles, int splits, hipStream_t st) {
-    constexpr int bytes = S * ((BN + BT) * kQ + 512 * WN * WT);
-    static_assert(bytes <= 160 * 1024);
-    const auto kernel = tiled_kernel<M, F32, BN, BT, WN, WT, S>;
-    static std::atomic<uint64_t> ready{0};   // devices whose LDS limit is raised
+// One launch of `kernel` with `bytes` of LDS; `ready`: devices whose limit is raised
+template <typename K>
+hipError_t launch_lds(K kernel, std::atomic<uint64_t> &ready, int bytes, int64_t grid, int threads,
+                      hipStream_t st, const ProductArgs &p, int n_tiles, int splits) {
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
@@ -236,10 +288,20 @@ hipError_t launch_tiled(const ProductArgs &p, int t_tiles, int splits, hipStream
         if (e != hipSuccess) return e;
         if (dev < 64) ready.fetch_or(1ull << dev);
     }
-    const int n_tiles = cdiv(p.N, M == Mode::GateUp ? BN / 2 : BN);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)n_tiles * t_tiles * splits)), dim3(64 * WN * WT),
-                       bytes, st, p, n_tiles, splits);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), bytes, st, p, n_tiles, splits);
     return hipSuccess;
+}
+
+template <Mode M, bool F32, int BN, int BT, int WN, int WT, int S>
+hipError_t launch_tiled(const ProductArgs &p, int t_tiles, int splits, hipStream_t st) {
+    constexpr int stages = S * ((BN + BT) * kQ + 512 * WN * WT);
+    constexpr int end = M == Mode::GateUp ? BT * (kQ + 4 * WN) : F32 ? 0 : BN * BT * 2;
+    constexpr int bytes = stages > end ? stages : end;
+    static_assert(bytes <= 160 * 1024);
+    static std::atomic<uint64_t> ready{0};
+    const int n_tiles = cdiv(p.N, M == Mode::GateUp ? BN / 2 : BN);
+    return launch_lds(tiled_kernel<M, F32, BN, BT, WN, WT, S>, ready, bytes, (int64_t)n_tiles * t_tiles * splits,
+                      64 * WN * WT, st, p, n_tiles, splits);
 }
 
 }  // namespace fp8

@@ -35,12 +35,6 @@ __device__ __forceinline__ bool ahead(V xv, int xi, V yv, int yi) {
     return xv > yv || (xv == yv && xi < yi);
 }
 
-// LDS written by lanes of this wave is there for its other lanes
-__device__ __forceinline__ void wave_lds() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // Groups by the sum of their best one or two of `value` (of all experts, in the
 // wave's LDS): the kept ones as bits group * lanes, in `keep`.  64 / (a power of
 // two of at least that many groups) lanes share a group.  exact: what is in LDS
@@ -645,7 +639,7 @@ int echo_moe_experts(const echo_experts_t *m, const void *x, const float *x_scal
     dn.KB = IB;
     dn.y = base + w.y;
     dn.y_stride = H;
-    dn.wide = true;   // H a multiple of 16, y the workspace's
+    dn.wide = dn.pieces = true;   // H a multiple of 16, y the workspace's
     const hipError_t e = w.tile == 128  ? run_experts<128, 4, 2, 3, 256, 4, 2, 3>(gu, dn, w.max_tiles, st)
                          : w.tile == 64 ? run_experts<64, 4, 2, 3, 128, 4, 1, 3>(gu, dn, w.max_tiles, st)
                          : w.tile == 32 ? run_experts<32, 4, 1, 2, 128, 4, 1, 3>(gu, dn, w.max_tiles, st)
