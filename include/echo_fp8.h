@@ -52,7 +52,8 @@ int echo_fp8_quantize(const void *x, int32_t x_dtype, int64_t x_stride, int32_t 
  * e4m3 matrix instructions add 128 products to about 1.5e-5 of the sum; an fp32
  * result takes exact products and fp32 sums).  residual (optional):
  * of y's type and strides, added before that rounding; it may be y itself, and
- * overlaps it in no other way.  K a multiple of 16; x and w 16-byte aligned.
+ * overlaps it in no other way; y overlaps no other buffer.  K a multiple of 16,
+ * at most 2^23; x and w 16-byte aligned.
  * workspace: device scratch of echo_fp8_gemm_workspace_bytes() bytes (may be
  * none), 256-byte aligned, used by no other call until this one has completed. */
 int echo_fp8_gemm(const void *x, const float *x_scale, const void *w, const float *w_scale,

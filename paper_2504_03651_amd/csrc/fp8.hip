@@ -269,7 +269,9 @@ void launch_rows(const ProductArgs &p, hipStream_t st) {
 
 template <bool F32, int BN, int BT, int WN, int WT, int S>
 hipError_t launch_tiles(const ProductArgs &p, int splits, hipStream_t st) {
-    return launch_tiled<Mode::Plain, F32, BN, BT, WN, WT, S>(p, cdiv(p.T, BT), splits, st);
+    if constexpr (BT <= 64)
+        if (p.T <= BT) return launch_tiled<Mode::Plain, F32, true, BN, BT, WN, WT, S>(p, 1, splits, st);
+    return launch_tiled<Mode::Plain, F32, false, BN, BT, WN, WT, S>(p, cdiv(p.T, BT), splits, st);
 }
 
 template <bool F32>
@@ -319,7 +321,7 @@ int check_sizes(int32_t T, int32_t N, int32_t K) {
     if (K % 16) return fail(ECHO_E_UNSUPPORTED, "in_features %d is not a multiple of 16", K);
     // offsets inside a tile are 32 bits, a grid's workgroups too
     if (K > 1 << 23) return fail(ECHO_E_UNSUPPORTED, "in_features %d above %d", K, 1 << 23);
-    if ((int64_t)cdiv(N, 16) * cdiv(T, 16) > INT32_MAX / 2 || N > INT32_MAX - 3)
+    if ((int64_t)cdiv(N, 16) * cdiv(T, 16) > INT32_MAX / 2 || N > 1 << 30 || T > 1 << 30)
         return fail(ECHO_E_UNSUPPORTED, "product of %d x %d too large", T, N);
     return ECHO_OK;
 }

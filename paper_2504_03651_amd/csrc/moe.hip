@@ -480,6 +480,10 @@ int plan_ws(const echo_experts_t *x, int32_t T, int32_t top_k, Ws *w) {
     if (top_k < 1 || top_k > kMaxTopK) return fail(ECHO_E_INVALID, "top_k %d (1..%d)", top_k, kMaxTopK);
     const int64_t R = (int64_t)T * top_k;
     if (R > 1 << 24) return fail(ECHO_E_UNSUPPORTED, "%lld pairs of token and expert", (long long)R);
+    // offsets of codes inside an expert's matrices and inside x are 32 bits
+    if (2 * (int64_t)x->intermediate * x->hidden > UINT32_MAX || (int64_t)T * x->hidden > UINT32_MAX)
+        return fail(ECHO_E_UNSUPPORTED, "more than 2^32 codes in an expert's matrix (%d x %d) or in x (%d x %d)",
+                    2 * x->intermediate, x->hidden, T, x->hidden);
     const int E = x->num_experts;
     // tiles of as many pairs as experts get on average
     // (measured either side, 64 experts of 2048 x 1024: 4 pairs an expert, 16 rows
@@ -514,10 +518,10 @@ int launched(const char *what) {
 // the down matrix, by the tile's pairs.
 template <int BT, int GN, int GT, int GS, int BN, int DN, int DT, int DS>
 hipError_t run_experts(const ProductArgs &gu, const ProductArgs &dn, int max_tiles, hipStream_t st) {
-    hipError_t e = launch_tiled<Mode::GateUp, false, 256, BT, GN, GT, GS>(gu, max_tiles, 1, st);
+    hipError_t e = launch_tiled<Mode::GateUp, false, (BT <= 64), 256, BT, GN, GT, GS>(gu, max_tiles, 1, st);
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return launch_tiled<Mode::Down, false, BN, BT, DN, DT, DS>(dn, max_tiles, 1, st);
+    return launch_tiled<Mode::Down, false, (BT <= 64), BN, BT, DN, DT, DS>(dn, max_tiles, 1, st);
 }
 
 }  // namespace

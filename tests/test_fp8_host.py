@@ -81,6 +81,7 @@ GEMM = dict(x=P, xs=P, w=P, ws=P, T=4, N=100, K=256, res=None, y=P, dtype=0, str
     (dict(w=at(4)), INV, "16-byte"), (dict(xs=at(2)), INV, "alignment"),
     (dict(y=at(1)), INV, "alignment"), (dict(dtype=1, res=at(2)), INV, "alignment"),
     (dict(T=2 ** 31 - 1, N=2 ** 31 - 1, stride=2 ** 31), UNS, "too large"),
+    (dict(T=1, N=2 ** 30 + 1, stride=2 ** 31), UNS, "too large"), (dict(K=2 ** 23 + 16), UNS, "above"),
 ])
 def test_gemm_refusals(change, code, what):
     rc = fp8._lib().echo_fp8_gemm(*{**GEMM, **change}.values(), P, 1 << 40, None)
@@ -142,6 +143,7 @@ CALL = dict(x=P, xs=P, T=5, top_k=2, ids=P, weights=P, residual=None, out=P)
     (dict(down_scale=at(2)), {}, INV, "aligned"),
     ({}, dict(T=-1), INV, "num_tokens"), ({}, dict(top_k=0), INV, "top_k"),
     ({}, dict(top_k=65), INV, "top_k"), ({}, dict(T=1 << 24), UNS, "pairs"),
+    (dict(hidden=1 << 16, intermediate=1 << 15), {}, UNS, "2^32"), (dict(hidden=1 << 12), dict(T=1 << 20), UNS, "2^32"),
     ({}, dict(x=None), INV, "NULL"), ({}, dict(xs=None), INV, "NULL"), ({}, dict(ids=None), INV, "NULL"),
     ({}, dict(weights=None), INV, "NULL"), ({}, dict(out=None), INV, "NULL"),
     ({}, dict(x=at(8)), INV, "16-byte"), ({}, dict(out=at(2)), INV, "16-byte"),
