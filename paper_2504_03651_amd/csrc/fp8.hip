@@ -7,7 +7,6 @@
 #include "echo_fp8.h"
 #include "fp8.hpp"
 #include "fp8_stream.hpp"
-#include "fp8_tiled.hpp"
 #include "status.hpp"
 
 namespace echo {
@@ -206,6 +205,14 @@ __global__ __launch_bounds__(256) void add_parts_kernel(ProductArgs p, int split
     store4<F32>(p, t, n, v);
 }
 
+// stages of a wave's ring, for NT = 1 and 2
+constexpr int rows_depth(int NT, int XR) { return XR == 8 ? (NT == 1 ? 5 : 3) : XR == 16 ? (NT == 1 ? 4 : 3) : NT == 1 ? 3 : 2; }
+constexpr int rows_tokens(int T) { return T <= 8 ? 8 : T <= 16 ? 16 : 32; }
+bool rows_fit(int NT, int T, int K) {
+    const int XR = rows_tokens(T);
+    return stream_bytes(NT, XR, rows_depth(NT, XR), cdiv(cdiv(K, kQ), kStreamWaves)) * kStreamWaves <= 160 * 1024;
+}
+
 // How a product is cut: the kernel's form, and how many ranges of K there are.
 enum Form { kRows16, kRows32, k64x32, k64x64, k128x64, k128x128, k256x128, k256x256 };
 struct Cut {
@@ -214,12 +221,11 @@ struct Cut {
 };
 
 // The cut of least estimated time, in microseconds fitted to 130 sizes (T 1 to
-// 4,640, N x K from 512 x 512 to 28672 x 4096, weights from memory); the cuts it
-// takes there cost 4% over the best of 21 forms x 8 splits in the geometric mean.
-//   A launch is 3.4.  Weights and tokens come at 5.2 TB/s at most.
-//   kRows: 16 or 32 weight rows a workgroup, straight into registers; a CU streams
-//   20 KB a microsecond, and less the more tokens' codes come beside them (8 x
-//   6144 x 4096: 10.2 by 32 rows, 12.1 by 16; x 4096 x 4096: 9.9 and 7.7).
+// 4,640, N x K from 512 x 512 to 28672 x 4096, weights from memory).
+//   Weights and tokens come at 5.2 TB/s at most.
+//   kRows: 16 or 32 weight rows a workgroup, every wave on its own; one workgroup a
+//   CU, which takes in 50 KB a microsecond, tokens among them (8 x 6144 x 4096: 9.0
+//   by 32 rows, 11.0 by 16; 8 x 4096 x 4096: 8.0 and 7.2).
 //   Tiles n x t: what a step of 128 of K takes with one workgroup on a CU, and
 //   with two where LDS holds two.
 //   Ranges of K cost a second launch and their fp32 parts' way to memory and back
@@ -230,9 +236,11 @@ Cut cut_of(int T, int N, int K) {
     Cut best{kRows16, 1};
     double least = 1e30;
     for (int nt = 1; nt <= 2; ++nt) {
-        const int64_t wgs = (int64_t)cdiv(N, 16 * nt) * cdiv(T, 32);
-        const double turn = 16.0 * nt * K / 20e3 * (1 + 0.035 * std::min(T, 32) / nt);
-        const double us = std::max(bytes / 5.2e6, turn * (1 + 0.6 * ((double)((wgs + 255) / 256) - 1)));
+        if (!rows_fit(nt, T, K)) continue;
+        const int x = rows_tokens(T);
+        const int64_t turns = ((int64_t)cdiv(N, 16 * nt) * cdiv(T, x > 16 ? 32 : 16) + 255) / 256;
+        const double us = std::max(bytes / 5.2e6, (double)turns * (16 * nt + x) * K / 50e3) + 0.6 +
+                          1.5 * (double)(turns - 1);
         if (us < least) least = us, best = Cut{nt == 1 ? kRows16 : kRows32, 1};
     }
     static const struct {
@@ -257,14 +265,15 @@ Cut cut_of(int T, int N, int K) {
     return best;
 }
 
-template <bool F32, int NT, int TT>
-void launch_rows(const ProductArgs &p, hipStream_t st) {
-    const int n_tiles = cdiv(p.N, 16 * NT);
-    const dim3 grid((unsigned)((int64_t)n_tiles * cdiv(p.T, 16 * TT))), block(512);
-    if (p.T <= 16 * TT)   // every weight read once
-        hipLaunchKernelGGL((stream_kernel<F32, true, NT, TT, 8, 4>), grid, block, 0, st, p, n_tiles);
-    else
-        hipLaunchKernelGGL((stream_kernel<F32, false, NT, TT, 8, 4>), grid, block, 0, st, p, n_tiles);
+template <bool F32, int NT>
+hipError_t launch_rows(const ProductArgs &p, hipStream_t st) {
+    switch (rows_tokens(p.T)) {   // up to 32 tokens every weight is read once
+        case 8: return launch_stream<F32, true, NT, 8, rows_depth(NT, 8)>(p, st);
+        case 16: return launch_stream<F32, true, NT, 16, rows_depth(NT, 16)>(p, st);
+        default:
+            return p.T <= 32 ? launch_stream<F32, true, NT, 32, rows_depth(NT, 32)>(p, st)
+                             : launch_stream<F32, false, NT, 32, rows_depth(NT, 32)>(p, st);
+    }
 }
 
 template <bool F32, int BN, int BT, int WN, int WT, int S>
@@ -278,14 +287,15 @@ template <bool F32>
 hipError_t launch_gemm(const ProductArgs &p, Cut c, hipStream_t st) {
     hipError_t e = hipSuccess;
     switch (c.form) {
-        case kRows16: p.T > 16 ? launch_rows<F32, 1, 2>(p, st) : launch_rows<F32, 1, 1>(p, st); return e;
-        case kRows32: p.T > 16 ? launch_rows<F32, 2, 2>(p, st) : launch_rows<F32, 2, 1>(p, st); return e;
+        case kRows16: return launch_rows<F32, 1>(p, st);
+        case kRows32: return launch_rows<F32, 2>(p, st);
         case k64x32: e = launch_tiles<F32, 64, 32, 4, 1, 5>(p, c.splits, st); break;
         case k64x64: e = launch_tiles<F32, 64, 64, 4, 1, 4>(p, c.splits, st); break;
-        case k128x64: e = launch_tiles<F32, 128, 64, 4, 1, 3>(p, c.splits, st); break;
         default:
-            // fp32 results, which take twice the products, in tiles of 128 x 128
-            if (F32 || c.form == k128x128) e = launch_tiles<F32, 128, 128, 4, 2, 4>(p, c.splits, st);
+            // fp32 results, which take more instructions a product, in tiles of 128
+            // x 64 at most (1,024 x 6144 x 4096: 73 us, in tiles of 128 x 128 90)
+            if (F32 || c.form == k128x64) e = launch_tiles<F32, 128, 64, 4, 1, 3>(p, c.splits, st);
+            else if (c.form == k128x128) e = launch_tiles<false, 128, 128, 4, 2, 4>(p, c.splits, st);
             else if (c.form == k256x128) e = launch_tiles<false, 256, 128, 4, 2, 3>(p, c.splits, st);
             else e = launch_tiles<false, 256, 256, 2, 4, 2>(p, c.splits, st);
     }

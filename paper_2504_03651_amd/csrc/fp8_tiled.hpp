@@ -282,19 +282,20 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
     finish<M, F32, BN, BT, WN, WT>(p, lds, acc, n_tiles, nb, n0, row0, rows, splits, split);
 }
 
-// One launch of `kernel` with `bytes` of LDS; `ready`: devices whose limit is raised
+// One launch of `kernel` with `bytes` of LDS, of `most` that it may ask for;
+// `ready`: devices whose limit is raised
 template <typename K>
-hipError_t launch_lds(K kernel, std::atomic<uint64_t> &ready, int bytes, int64_t grid, int threads,
-                      hipStream_t st, const ProductArgs &p, int n_tiles, int splits) {
+hipError_t launch_lds(K kernel, std::atomic<uint64_t> &ready, int most, int bytes, int64_t grid, int threads,
+                      hipStream_t st, const ProductArgs &p, int n_tiles, int last) {
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (dev >= 64 || !(ready.load() >> dev & 1)) {
-        e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, most);
         if (e != hipSuccess) return e;
         if (dev < 64) ready.fetch_or(1ull << dev);
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), bytes, st, p, n_tiles, splits);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), bytes, st, p, n_tiles, last);
     return hipSuccess;
 }
 
@@ -306,7 +307,7 @@ hipError_t launch_tiled(const ProductArgs &p, int t_tiles, int splits, hipStream
     static_assert(bytes <= 160 * 1024);
     static std::atomic<uint64_t> ready{0};
     const int n_tiles = cdiv(p.N, M == Mode::GateUp ? BN / 2 : BN);
-    return launch_lds(tiled_kernel<M, F32, ONCE, BN, BT, WN, WT, S>, ready, bytes, (int64_t)n_tiles * t_tiles * splits,
+    return launch_lds(tiled_kernel<M, F32, ONCE, BN, BT, WN, WT, S>, ready, bytes, bytes, (int64_t)n_tiles * t_tiles * splits,
                       64 * WN * WT, st, p, n_tiles, splits);
 }
 
