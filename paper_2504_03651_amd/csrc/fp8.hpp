@@ -18,11 +18,14 @@ __host__ __device__ inline int cdiv(int64_t a, int64_t b) { return (int)((a + b 
 
 __device__ __forceinline__ float bf2f(uint32_t b) { return __uint_as_float(b << 16); }
 
-// fp32 -> bf16, round to nearest even (NaN stays a quiet NaN)
-__device__ __forceinline__ uint32_t f2bf(float x) {
-    const uint32_t u = __float_as_uint(x);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0x7FC0;
-    return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// fp32 -> bf16, round to nearest even (a NaN stays one): one instruction
+__device__ __forceinline__ uint32_t f2bf(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ uint32_t f2bf2(float x, float y) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x, y}, bf16x2));
 }
 
 // Two fp32 -> two e4m3fn codes in the low 16 bits, round to nearest even,
@@ -40,9 +43,6 @@ __device__ __forceinline__ float scale_of(float amax) {
     const float s = amax / 448.0f;
     return s == 0.f ? 1.f : s;
 }
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // Eight e4m3 codes as bf16, exact (every e4m3 value is a bf16 value)
 __device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
@@ -144,7 +144,7 @@ __device__ __forceinline__ void store4(const ProductArgs &p, int64_t t, int n, f
                 for (int r = 0; r < 2; ++r) v[2 * r] += bf2f(q[r] & 0xFFFFu), v[2 * r + 1] += bf2f(q[r] >> 16);
             }
             *(u32x2 *)((uint16_t *)p.y + at) =
-                (u32x2){f2bf(v[0]) | (f2bf(v[1]) << 16), f2bf(v[2]) | (f2bf(v[3]) << 16)};
+                (u32x2){f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
         }
         return;
     }

@@ -129,13 +129,13 @@ __global__ __launch_bounds__(64 * kStreamWaves) void stream_kernel(ProductArgs p
 
 template <bool F32, bool ONCE, int NT, int XR, int D>
 hipError_t launch_stream(const ProductArgs &p, hipStream_t st) {
-    static std::atomic<uint64_t> ready{0};
+    static std::atomic<int> resident[64];
     const int n_tiles = cdiv(p.N, 16 * NT), t_tiles = cdiv(p.T, XR > 16 ? 32 : 16);
     const int wave_bytes = stream_bytes(NT, XR, D, cdiv(p.KB, kStreamWaves));
     const int sums = kStreamWaves * NT * (XR > 16 ? 2 : 1) * 1024;
     const int bytes = wave_bytes * kStreamWaves > sums ? wave_bytes * kStreamWaves : sums;
-    return launch_lds(stream_kernel<F32, ONCE, NT, XR, D>, ready, 160 * 1024, bytes, (int64_t)n_tiles * t_tiles,
-                      64 * kStreamWaves, st, p, n_tiles, wave_bytes);
+    return launch_lds(stream_kernel<F32, ONCE, NT, XR, D>, resident, 160 * 1024, bytes, (int64_t)n_tiles * t_tiles,
+                      false, 64 * kStreamWaves, st, p, n_tiles, wave_bytes);
 }
 
 }  // namespace fp8

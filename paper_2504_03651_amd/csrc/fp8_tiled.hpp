@@ -1,6 +1,9 @@
 // fp8_tiled.hpp -- e4m3 products for many tokens: operand tiles in LDS.
 #pragma once
 
+#include <algorithm>
+#include <atomic>
+
 #include "fp8.hpp"
 
 namespace echo {
@@ -21,16 +24,19 @@ __device__ __forceinline__ void landed_but() {
 // What a tile's workgroup does with its sums.  Results of 16 bits and codes go
 // through LDS, so that a store instruction writes whole pieces of rows: the tile
 // has them by columns, four values of a row a lane.
-// Uses at most BN * BT * 2 bytes of LDS (GateUp: BT * (128 + 4 WN)).
-template <Mode M, bool F32, int BN, int BT, int WN, int WT>
+// Uses at most ROOM bytes of LDS, in PASSES where the whole tile needs more.
+template <Mode M, bool F32, int BN, int BT, int WN, int WT, int ROOM>
 __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
                                        f32x4 (&acc)[BN / WN / 16][BT / WT / 16], int n_tiles, int nb,
                                        int n0, int row0, int rows, int splits, int split) {
     constexpr int NW = BN / WN, TW = BT / WT, NI = NW / 16, NJ = TW / 16;
-    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));   // addresses are computed here, not kept over the steps
+    const int g = lane >> 4, c = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave % WN, wt = wave / WN;
     if constexpr (M == Mode::GateUp) {
+        static_assert(BT * (kQ + 4 * WN) <= ROOM);
         float *peak = (float *)(lds + BT * kQ);   // [WN][BT]
         __syncthreads();   // the last step's reads are done
 #pragma unroll
@@ -40,9 +46,12 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
             for (int i = 0; i < NI / 2; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
+                    // a / (1 + e^-a) u; columns past N repeat the last one.  The
+                    // exponential is |a| 2^-24 off, the reciprocal 2^-23: no
+                    // more than the sums behind a, under codes of 2^-4.
                     const float a = acc[i][j][r];
-                    const float h = n0 + wn * (NW / 2) + 16 * i < p.N
-                                        ? a / (1.f + expf(-a)) * acc[NI / 2 + i][j][r] : 0.f;
+                    const float h = a * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * a)) *
+                                    acc[NI / 2 + i][j][r];
                     acc[i][j][r] = h;
                     m = fmaxf(m, fabsf(h));   // a NaN keeps out
                 }
@@ -59,15 +68,28 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
             for (int v = 1; v < WN; ++v) m = fmaxf(m, peak[v * BT + r]);
             const float s = scale_of(m);
             if (wn == 0 && g == 0 && r < rows) p.hs[(int64_t)(row0 + r) * n_tiles + nb] = s;
-            // h / s by the reciprocal, both times 2^64 where that could overflow
-            const float f = s < 0x1p-64f ? 0x1p64f : 1.f, inv = 1.f / (s * f);
+            // h / s by the reciprocal: at most 448 (1 + 2^-21), which rounds to 448,
+            // but for scales below 2^-126, which are coarser than that
+            float inv = __builtin_amdgcn_rcpf(s);
+            if (s < 0x1p-100f) {
+                inv = 1.f / (s * 0x1p64f);
+#pragma unroll
+                for (int i = 0; i < NI / 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float h = acc[i][j][e] * 0x1p64f * inv;
+                        acc[i][j][e] = h > 448.f ? 448.f : h < -448.f ? -448.f : h;
+                    }
+                inv = 1.f;
+            }
 #pragma unroll
             for (int i = 0; i < NI / 2; ++i) {
-                const f32x4 h = acc[i][j] * f * inv;
+                const f32x4 h = acc[i][j] * inv;
                 // 16-byte piece q of row r at place q ^ (r & 7)
                 const int at = wn * (NW / 2) + 16 * i + 4 * g;
                 *(uint32_t *)(lds + r * kQ + 16 * ((at >> 4) ^ (r & 7)) + (at & 15)) =
-                    e4m3x2(h[0], h[1]) | (e4m3x2(h[2], h[3]) << 16);
+                    __builtin_amdgcn_cvt_pk_fp8_f32(
+                        h[2], h[3], __builtin_amdgcn_cvt_pk_fp8_f32(h[0], h[1], 0, false), true);
             }
         }
         __syncthreads();
@@ -96,35 +118,42 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
         }
     } else {
         constexpr int Q = NW / 8;   // 16-byte pieces of a row of this wave
-        uint8_t *mine = lds + wave * (NW * TW * 2);
+        constexpr int PASSES = (BN * BT * 2 + ROOM - 1) / ROOM, TP = TW / PASSES;
+        static_assert(TP % 16 == 0 && TP * PASSES == TW);
+        uint8_t *mine = lds + wave * (NW * TP * 2);
         __syncthreads();   // the last step's reads are done
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int r = 16 * j + c;
-            const bool live = wt * TW + r < rows;
+        for (int pass = 0; pass < PASSES; ++pass) {
+            const int t0 = wt * TW + pass * TP;   // the pass's first row
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                f32x4 v = acc[i][j];
-                const int n = 16 * i + 4 * g;
-                if (M == Mode::Plain && p.residual && live && n0 + wn * NW + n < p.N) {
-                    const u32x2 q = *(const u32x2 *)((const uint16_t *)p.residual +
-                                                     (row0 + wt * TW + r) * p.y_stride + n0 + wn * NW + n);
+            for (int j = 0; j < TP / 16; ++j) {
+                const int r = 16 * j + c;
+                const bool live = t0 + r < rows;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) v[2 * e] += bf2f(q[e] & 0xFFFFu), v[2 * e + 1] += bf2f(q[e] >> 16);
+                for (int i = 0; i < NI; ++i) {
+                    f32x4 v = acc[i][pass * (TP / 16) + j];
+                    const int n = 16 * i + 4 * g;
+                    if (M == Mode::Plain && p.residual && live && n0 + wn * NW + n < p.N) {
+                        const u32x2 q = *(const u32x2 *)((const uint16_t *)p.residual +
+                                                         (row0 + t0 + r) * p.y_stride + n0 + wn * NW + n);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) v[2 * e] += bf2f(q[e] & 0xFFFFu), v[2 * e + 1] += bf2f(q[e] >> 16);
+                    }
+                    *(u32x2 *)(mine + (r * Q + ((n >> 3) ^ (r & (Q - 1)))) * 16 + (n & 4) * 2) =
+                        (u32x2){f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
                 }
-                *(u32x2 *)(mine + (r * Q + ((n >> 3) ^ (r & (Q - 1)))) * 16 + (n & 4) * 2) =
-                    (u32x2){f2bf(v[0]) | (f2bf(v[1]) << 16), f2bf(v[2]) | (f2bf(v[3]) << 16)};
             }
-        }
-        wave_lds();
-        const int q = lane % Q, n = n0 + wn * NW + 8 * q;
+            wave_lds();
+            const int q = lane % Q, n = n0 + wn * NW + 8 * q;
 #pragma unroll
-        for (int r0 = 0; r0 < TW; r0 += 64 / Q) {
-            const int r = r0 + lane / Q, row = wt * TW + r;
-            if (row >= rows || n >= p.N) continue;
-            const int64_t t = M == Mode::Down ? p.order[row0 + row] : row0 + row;
-            *(u32x4 *)((uint16_t *)p.y + t * p.y_stride + n) =
-                *(const u32x4 *)(mine + (r * Q + (q ^ (r & (Q - 1)))) * 16);
+            for (int r0 = 0; r0 < TP; r0 += 64 / Q) {
+                const int r = r0 + lane / Q, row = t0 + r;
+                if (row >= rows || n >= p.N) continue;
+                const int64_t t = M == Mode::Down ? p.order[row0 + row] : row0 + row;
+                *(u32x4 *)((uint16_t *)p.y + t * p.y_stride + n) =
+                    *(const u32x4 *)(mine + (r * Q + (q ^ (r & (Q - 1)))) * 16);
+            }
+            if (pass + 1 < PASSES) wave_lds();
         }
     }
 }
@@ -144,7 +173,7 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
 // part: fp32 sums of one of `splits` equal ranges of K go to part[split][t][n],
 // rows part_pitch apart, instead of y.
 template <Mode M, bool F32, bool ONCE, int BN, int BT, int WN, int WT, int S>
-__global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n_tiles, int splits) {
+__global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n_tiles, int t_tiles, int splits) {
     constexpr int W = WN * WT, NW = BN / WN, TW = BT / WT;   // a wave's rows and tokens
     constexpr int NI = NW / 16, NJ = TW / 16;
     constexpr int CODES = (BN + BT) * kQ, STAGE = CODES + 512 * W;
@@ -157,59 +186,69 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave % WN, wt = wave / WN;
 
-    int b = blockIdx.x;
-    const int split = b % splits;
-    b /= splits;
-    const int ti = b / n_tiles, nb = b - ti * n_tiles;
-    const int kb0 = (int)((int64_t)p.KB * split / splits), kb1 = (int)((int64_t)p.KB * (split + 1) / splits);
-    int row0 = BT * ti, rows = min(BT, p.T - row0);
-    const uint8_t *wbase = p.w;
-    const float *sbase = p.ws;
-    if constexpr (M != Mode::Plain) {
-        if (ti >= *p.num_tiles) return;
-        const Tile t = p.tiles[ti];
-        row0 = t.row0;
-        rows = t.rows;
-        wbase += t.expert * p.w_expert;
-        sbase += t.expert * p.ws_expert;
-    }
-    const int n0 = (M == Mode::GateUp ? BN / 2 : BN) * nb;
-
-    // sources of this lane's copies, in bytes from the tile's weights (rows of
-    // the stage below BN) and from its tokens
-    const uint8_t *wsrc = wbase, *xsrc = p.x;
-    const float *xscale = p.xs;
-    if constexpr (M != Mode::GateUp) {
-        wsrc += (int64_t)n0 * p.K;
-        xsrc += (int64_t)row0 * p.K;
-        xscale += (int64_t)row0 * p.KB;
-    }
-    const int piece = (lane & 7) ^ (lane >> 3);
-    auto token = [&](int r) -> uint32_t {   // row of x that the tile's row r reads
-        r = min(r, rows - 1);
-        return M == Mode::GateUp ? (uint32_t)(p.order[row0 + r] / p.top_k) : (uint32_t)r;
-    };
     // copies of a wave: COPIES, or one less where the stage's pieces run out
     const bool more = EXTRA == 0 || wave < EXTRA;
-    uint32_t src[COPIES];
-#pragma unroll
-    for (int i = 0; i < COPIES; ++i) {
-        const int r = min(8 * (W * i + wave), BN + BT - 8) + (lane >> 3);
-        uint32_t row;
-        if (W * i + wave >= BN / 8) {
-            row = token(r - BN);
-        } else if constexpr (M == Mode::GateUp) {
-            const int q = r % NW, n = min(n0 + (r / NW) * (NW / 2) + q % (NW / 2), p.N - 1);
-            row = q < NW / 2 ? n : p.N + n;
+    const int piece = (lane & 7) ^ (lane >> 3);
+    const int units = (M == Mode::Plain ? t_tiles : *p.num_tiles) * n_tiles * splits;
+    // The unit of work: rows n0 .. of the weights by rows row0 .. of the tokens,
+    // steps kb0 to kb1; and the sources of this lane's copies, in bytes from the
+    // tile's weights (rows of the stage below BN) and from its tokens.
+    int split, nb, n0, row0, rows, kb0, kb1;
+    const uint8_t *wsrc, *xsrc;
+    const float *xscale, *ws;   // ws: lanes below 32 the (gate) rows' scales, above the up rows'
+    uint32_t src[COPIES], xs;
+    auto take = [&](int b) {
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));   // computed here, not kept over the steps
+        const int piece = (lane & 7) ^ (lane >> 3);
+        split = b % splits;
+        b /= splits;
+        const int ti = b / n_tiles;
+        nb = b - ti * n_tiles;
+        n0 = (M == Mode::GateUp ? BN / 2 : BN) * nb;
+        kb0 = (int)((int64_t)p.KB * split / splits);
+        kb1 = (int)((int64_t)p.KB * (split + 1) / splits);
+        wsrc = p.w;
+        const float *sbase = p.ws;
+        if constexpr (M == Mode::Plain) {
+            row0 = BT * ti;
+            rows = min(BT, p.T - row0);
         } else {
-            row = min(r, p.N - 1 - n0);
+            const Tile t = p.tiles[ti];
+            row0 = t.row0;
+            rows = t.rows;
+            wsrc += t.expert * p.w_expert;
+            sbase += t.expert * p.ws_expert;
         }
-        src[i] = row * (uint32_t)p.K + 16 * piece;
-    }
-    const uint32_t xs = token(wt * TW + lane % TW) * (uint32_t)p.KB;
-    const float *ws;   // lanes below 32: the (gate) rows' scales, above: the up rows'
-    if constexpr (M == Mode::GateUp) ws = sbase + (int64_t)(lane < 32 ? nb : n_tiles + nb) * p.KB;
-    else ws = sbase + (int64_t)min((n0 + wn * NW) / kQ, (p.N - 1) / kQ) * p.KB;
+        xsrc = p.x;
+        xscale = p.xs;
+        if constexpr (M != Mode::GateUp) {
+            wsrc += (int64_t)n0 * p.K;
+            xsrc += (int64_t)row0 * p.K;
+            xscale += (int64_t)row0 * p.KB;
+        }
+        auto token = [&](int r) -> uint32_t {   // row of x that the tile's row r reads
+            r = min(r, rows - 1);
+            return M == Mode::GateUp ? (uint32_t)p.order[row0 + r] / (uint32_t)p.top_k : (uint32_t)r;
+        };
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const int r = min(8 * (W * i + wave), BN + BT - 8) + (lane >> 3);
+            uint32_t row;
+            if (W * i + wave >= BN / 8) {
+                row = token(r - BN);
+            } else if constexpr (M == Mode::GateUp) {
+                const int q = r % NW, n = min(n0 + (r / NW) * (NW / 2) + q % (NW / 2), p.N - 1);
+                row = q < NW / 2 ? n : p.N + n;
+            } else {
+                row = min(r, p.N - 1 - n0);
+            }
+            src[i] = row * (uint32_t)p.K + 16 * piece;
+        }
+        xs = token(wt * TW + lane % TW) * (uint32_t)p.KB;
+        if constexpr (M == Mode::GateUp) ws = sbase + (int64_t)(lane < 32 ? nb : n_tiles + nb) * p.KB;
+        else ws = sbase + (int64_t)min((n0 + wn * NW) / kQ, (p.N - 1) / kQ) * p.KB;
+    };
     auto copy = [&](int kb, int slot) {
         uint8_t *stage = lds + slot * STAGE, *dst = stage + 1024 * wave;
         const uint8_t *w = wsrc + (int64_t)kQ * kb, *x = xsrc + (int64_t)kQ * kb;
@@ -234,17 +273,23 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
         else landed_but<AHEAD * (COPIES + 1)>();
     };
 
+    const int at = 16 * (g ^ (c & 7));   // place of piece g; piece g + 4 at the same ^ 64
+    int slot = 0;
+    auto start = [&] {
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i)
+            if (kb0 + i < kb1) copy(kb0 + i, slot + i < S ? slot + i : slot + i - S);
+    };
+    int unit = blockIdx.x;
+    if (unit >= units) return;
+    take(unit);
+    start();
+    while (true) {
     f32x4 acc[NI][NJ];
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
-
-    const int at = 16 * (g ^ (c & 7));   // place of piece g; piece g + 4 at the same ^ 64
-#pragma unroll
-    for (int i = 0; i < S - 1; ++i)
-        if (kb0 + i < kb1) copy(kb0 + i, i);
-    int slot = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
         landed(kb);
         const int free = slot == 0 ? S - 1 : slot - 1;
@@ -279,36 +324,52 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
         slot = slot + 1 == S ? 0 : slot + 1;
     }
 
-    finish<M, F32, BN, BT, WN, WT>(p, lds, acc, n_tiles, nb, n0, row0, rows, splits, split);
+    // the next unit's first steps go to the stages that the last step left free,
+    // and this one's results through the last step's
+    uint8_t *last = lds + (slot == 0 ? S - 1 : slot - 1) * STAGE;
+    const int nb_ = nb, n0_ = n0, row0_ = row0, rows_ = rows, split_ = split;
+    unit += gridDim.x;
+    const bool again = unit < units;
+    if (again) {
+        take(unit);
+        start();
+    }
+    finish<M, F32, BN, BT, WN, WT, STAGE>(p, last, acc, n_tiles, nb_, n0_, row0_, rows_, splits, split_);
+    if (!again) break;
+    }
 }
 
 // One launch of `kernel` with `bytes` of LDS, of `most` that it may ask for;
-// `ready`: devices whose limit is raised
-template <typename K>
-hipError_t launch_lds(K kernel, std::atomic<uint64_t> &ready, int most, int bytes, int64_t grid, int threads,
-                      hipStream_t st, const ProductArgs &p, int n_tiles, int last) {
+// `resident`: of each device, the workgroups that it holds at once, once `most` is set
+template <typename K, typename... A>
+hipError_t launch_lds(K kernel, std::atomic<int> (&resident)[64], int most, int bytes, int64_t grid, bool loops,
+                      int threads, hipStream_t st, A... args) {
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
-    if (dev >= 64 || !(ready.load() >> dev & 1)) {
+    int at_once = dev < 64 ? resident[dev].load() : 0;
+    if (!at_once) {
+        int cus = 0, per = 0;
         e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+        if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+        if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per, (const void *)kernel, threads, bytes);
         if (e != hipSuccess) return e;
-        if (dev < 64) ready.fetch_or(1ull << dev);
+        at_once = std::max(1, cus * per);
+        if (dev < 64) resident[dev].store(at_once);
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), bytes, st, p, n_tiles, last);
+    if (loops) grid = std::min<int64_t>(grid, at_once);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), bytes, st, args...);
     return hipSuccess;
 }
 
 template <Mode M, bool F32, bool ONCE, int BN, int BT, int WN, int WT, int S>
 hipError_t launch_tiled(const ProductArgs &p, int t_tiles, int splits, hipStream_t st) {
-    constexpr int stages = S * ((BN + BT) * kQ + 512 * WN * WT);
-    constexpr int end = M == Mode::GateUp ? BT * (kQ + 4 * WN) : F32 ? 0 : BN * BT * 2;
-    constexpr int bytes = stages > end ? stages : end;
+    constexpr int bytes = S * ((BN + BT) * kQ + 512 * WN * WT);
     static_assert(bytes <= 160 * 1024);
-    static std::atomic<uint64_t> ready{0};
+    static std::atomic<int> resident[64];
     const int n_tiles = cdiv(p.N, M == Mode::GateUp ? BN / 2 : BN);
-    return launch_lds(tiled_kernel<M, F32, ONCE, BN, BT, WN, WT, S>, ready, bytes, bytes, (int64_t)n_tiles * t_tiles * splits,
-                      64 * WN * WT, st, p, n_tiles, splits);
+    return launch_lds(tiled_kernel<M, F32, ONCE, BN, BT, WN, WT, S>, resident, bytes, bytes,
+                      (int64_t)n_tiles * t_tiles * splits, true, 64 * WN * WT, st, p, n_tiles, t_tiles, splits);
 }
 
 }  // namespace fp8

@@ -449,7 +449,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const uint16_t *y, const i
     }
     u32x4 o;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) o[r] = f2bf(v[2 * r]) | (f2bf(v[2 * r + 1]) << 16);
+    for (int r = 0; r < 4; ++r) o[r] = f2bf2(v[2 * r], v[2 * r + 1]);
     *(u32x4 *)(out + t * H + h) = o;
 }
 
