@@ -35,18 +35,19 @@ __device__ __forceinline__ bool ahead(V xv, int xi, V yv, int yi) {
     return xv > yv || (xv == yv && xi < yi);
 }
 
-// Groups by the sum of their best one or two of `value` (of all experts, in the
-// wave's LDS): the kept ones as bits group * lanes, in `keep`.  64 / (a power of
-// two of at least that many groups) lanes share a group.  exact: what is in LDS
-// decides; otherwise returns whether the last kept group is more than `apart`
-// times (1 + its magnitude) ahead of the first dropped one.
-template <typename V>
+// Of each token, LANES lanes of the wave: groups by the sum of their best one or
+// two of `value` (of all experts, in LDS): the kept ones as bits group * lanes, in
+// `keep`.  LANES / (a power of two of at least that many groups) = `lanes` lanes share
+// a group.  exact: what is in LDS decides; otherwise returns whether the last kept
+// group is more than `apart` times (1 + its magnitude) ahead of the first dropped one.
+template <int LANES, typename V>
 __device__ __forceinline__ bool keep_groups(const RouteArgs &a, const V *value, int lanes, int lane,
                                             bool exact, V apart, uint64_t &keep) {
-    const int per = a.E / a.groups, g = lane / lanes, sub = lane & (lanes - 1);
+    const int sub = lane & (LANES - 1), from = lane & ~(LANES - 1);
+    const int per = a.E / a.groups, g = sub / lanes, in = sub & (lanes - 1);
     V b1 = -INFINITY, b2 = -INFINITY;
     if (g < a.groups)
-        for (int j = sub; j < per; j += lanes) {
+        for (int j = in; j < per; j += lanes) {
             const V k = value[g * per + j];
             b2 = k > b1 ? b1 : k > b2 ? k : b2;
             b1 = k > b1 ? k : b1;
@@ -60,17 +61,22 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs &a, const V *value, 
     V v = a.group_top == 2 ? b1 + b2 : b1;
     if (sizeof(V) == 8 && v > (V)DBL_MAX) v = (V)DBL_MAX;
     int rank = 0;
-    for (int j = 0; j < a.groups; ++j) rank += ahead(__shfl(v, j * lanes), j, v, g);
-    keep = __ballot(sub == 0 && g < a.groups && rank < a.top_groups);
+    for (int j = 0; j < a.groups; ++j) rank += ahead(__shfl(v, from + j * lanes), j, v, g);
+    auto of = [&](bool x) -> uint64_t {   // this token's lanes where x holds of a group
+        const uint64_t m = __ballot(in == 0 && g < a.groups && x) >> from;
+        return LANES == 64 ? m : m & ((1ull << (LANES & 63)) - 1);
+    };
+    keep = of(rank < a.top_groups);
     if (exact || a.top_groups == a.groups) return true;
-    const V last = __shfl(v, __ffsll((long long)__ballot(sub == 0 && g < a.groups && rank == a.top_groups - 1)) - 1);
-    const V next = __shfl(v, __ffsll((long long)__ballot(sub == 0 && g < a.groups && rank == a.top_groups)) - 1);
+    const V last = __shfl(v, from + __ffsll((long long)of(rank == a.top_groups - 1)) - 1);
+    const V next = __shfl(v, from + __ffsll((long long)of(rank == a.top_groups)) - 1);
     return last - next > apart * (1 + (last < 0 ? -last : last));
 }
 
+template <int LANES>
 __device__ __forceinline__ int lanes_of_group(int groups) {
-    int l = 64;
-    while (64 / l < groups) l >>= 1;
+    int l = LANES;
+    while (LANES / l < groups) l >>= 1;
     return l;
 }
 
@@ -78,7 +84,7 @@ __device__ __forceinline__ int lanes_of_group(int groups) {
 // id and weight of lane j: of the row's j-th expert.
 template <bool F32, bool SIGMOID, int PER>
 __device__ __forceinline__ void route_row64(const RouteArgs &a, int64_t t, double *row, int lane,
-                                                      int &id, float &weight) {
+                                            int &id, float &weight) {
     double score[PER], key[PER];
     double top = -DBL_MAX;
 #pragma unroll
@@ -118,7 +124,7 @@ __device__ __forceinline__ void route_row64(const RouteArgs &a, int64_t t, doubl
         }
     }
     if (a.groups > 1) {
-        const int per = a.E / a.groups, lanes = lanes_of_group(a.groups);
+        const int per = a.E / a.groups, lanes = lanes_of_group<64>(a.groups);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = lane + 64 * i;
@@ -127,7 +133,7 @@ __device__ __forceinline__ void route_row64(const RouteArgs &a, int64_t t, doubl
         }
         wave_lds();
         uint64_t keep;
-        keep_groups<double>(a, row, lanes, lane, true, 0.0, keep);
+        keep_groups<64, double>(a, row, lanes, lane, true, 0.0, keep);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = lane + 64 * i;
@@ -165,51 +171,58 @@ __device__ __forceinline__ int ordered(float x) {
 }
 __device__ __forceinline__ float unordered(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
 
-// max over the wave: rotations in rows of 16 lanes, then swaps of rows and halves
-__device__ __forceinline__ int wave_max(int v) {
+// max over LANES lanes: rotations in rows of 16, then swaps of rows and halves
+template <int LANES>
+__device__ __forceinline__ int lanes_max(int v) {
     v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, false));   // row_ror:8
     v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xF, 0xF, false));
     v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xF, 0xF, false));
     v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xF, 0xF, false));
+    if constexpr (LANES == 16) return v;
     const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
     v = max((int)a[0], (int)a[1]);
     const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
     return __builtin_amdgcn_readfirstlane(max((int)b[0], (int)b[1]));
 }
 
-// One wave per token; lane l has experts l, l + 64, ...  Without a bias the keys
-// are the logits, exact in fp32.  With one (or where groups go by sums of scores)
-// the keys come in fp32, off by less than off (1 + |key|): for a sigmoid s, s (1 -
-// s) 2^-23 from the exponential and 2^-24 s each from the sum and the quotient, with
-// the rounding of the key below 4 x 2^-24; for a softmax at most 20 roundings of a
-// score (its exponential's, the sum's over the lanes, the reciprocal's), below
-// 2^-19.  Where two neighbours among the chosen and the next, or the groups at
-// the border, are not further apart than that the row goes to route_row64.  The
-// chosen experts' scores are taken in 64 bits.  16,412 tokens of 256 experts with
-// groups and bias take 32 us (60 all in 64 bits), bound by instructions: nine
-// maxima over the wave and what finds them.
-
-template <bool F32, bool SIGMOID, int PER>
+// LANES lanes of a wave per token; lane l of them has experts l, l + LANES, ...
+// Without a bias the keys are the logits, exact in fp32.  With one (or where groups
+// go by sums of scores) the keys come in fp32, off by less than off (1 + |key|): for
+// a sigmoid s = 1 / (1 + e), e = e^-z comes (|z| + 2) 2^-24 off, which makes s (1 - s)
+// (|z| + 2) 2^-24 < 0.75 x 2^-24 of it, the sum and the hardware's reciprocal 3 x
+// 2^-24 s, with the rounding of the key below 5 x 2^-24; for a softmax at most 20
+// roundings of a score (its exponential's, the sum's over the lanes, the
+// reciprocal's), below 2^-19.  Where two neighbours among the chosen and the next,
+// or the groups at the border, are not further apart than that the row goes to
+// route_row64.  The chosen experts' scores are taken in 64 bits.
+// Bound by instructions, and where rows go to route_row64 by its 8 us: 16,412 tokens
+// of 256 experts, 8 chosen of 4 groups of 8 with a bias, take 27 us (34 with a wave
+// a token).
+template <bool F32, bool SIGMOID, int PER, int LANES>
 __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
     extern __shared__ double route_lds[];
-    const int lane = threadIdx.x & 63;
+    static_assert(LANES == 16 || LANES == 64);
+    constexpr int TOKENS = 64 / LANES;   // of a wave
+    const int lane = threadIdx.x & 63, sub = lane & (LANES - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t t = (int64_t)blockIdx.x * 4 + wave;
-    if (t >= a.T) return;
-    constexpr float off = SIGMOID ? 0x1p-22f : 0x1p-19f;
-    double *row = route_lds + wave * (a.groups > 1 ? a.E : 0);
+    const int64_t t0 = ((int64_t)blockIdx.x * 4 + wave) * TOKENS;
+    if (t0 >= a.T) return;
+    const int64_t t = min(t0 + lane / LANES, (int64_t)a.T - 1);
+    constexpr float off = SIGMOID ? 0x1p-21f : 0x1p-19f;
+    // of a wave: E doubles, or E floats of each token
+    double *row = route_lds + wave * (a.groups > 1 ? a.E * (TOKENS > 1 ? TOKENS / 2 : 1) : 0);
     float z[PER];
     int key[PER];
     const int none = ordered(-INFINITY);
+    auto logit = [&](int64_t t, int e) {
+        const int64_t at = t * a.stride + e;
+        const float f = F32 ? ((const float *)a.logits)[at] : bf2f(((const uint16_t *)a.logits)[at]);
+        return f > -INFINITY ? fminf(f, FLT_MAX) + 0.f : -INFINITY;   // NaN too; -0 becomes 0
+    };
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int e = lane + 64 * i;
-        z[i] = -INFINITY;
-        if (e < a.E) {
-            const int64_t at = t * a.stride + e;
-            const float f = F32 ? ((const float *)a.logits)[at] : bf2f(((const uint16_t *)a.logits)[at]);
-            if (f > -INFINITY) z[i] = fminf(f, FLT_MAX) + 0.f;   // not for NaN; -0 becomes 0
-        }
+        const int e = sub + LANES * i;
+        z[i] = e < a.E ? logit(t, e) : -INFINITY;
         key[i] = ordered(z[i]);
     }
     float top = 0.f;
@@ -217,14 +230,15 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
         int m = key[0];
 #pragma unroll
         for (int i = 1; i < PER; ++i) m = max(m, key[i]);
-        top = unordered(wave_max(m));
+        top = unordered(lanes_max<LANES>(m));
     }
     const bool sums = a.groups > 1 && a.group_top == 2 && !a.bias;   // groups by sums of scores
-    float sc[PER];
     if (a.bias || sums) {
+        float sc[PER];
         if constexpr (SIGMOID) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) sc[i] = 1.f / (1.f + expf(-z[i]));
+            for (int i = 0; i < PER; ++i)
+                sc[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z[i]));
         } else {
             float sum = 0.f;
 #pragma unroll
@@ -232,7 +246,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
                 sc[i] = z[i] == -INFINITY ? 0.f : expf(z[i] - top);
                 sum += sc[i];
             }
-            for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+            for (int o = 1; o < LANES; o <<= 1) sum += __shfl_xor(sum, o);
             const float r = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
             for (int i = 0; i < PER; ++i) sc[i] *= r;
@@ -240,95 +254,138 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
         if (a.bias) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const float k = sc[i] + a.bias[min(lane + 64 * i, a.E - 1)];
+                const float k = sc[i] + a.bias[min(sub + LANES * i, a.E - 1)];
                 key[i] = z[i] > -INFINITY && k > -INFINITY ? ordered(k) : none;   // not for NaN
             }
         }
-    }
-    bool sure = true;
-    if (a.groups > 1) {
-        float *value = (float *)row;
-        const int lanes = lanes_of_group(a.groups);
+        if (a.groups > 1) {
+            float *value = (float *)row + lane / LANES * a.E;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = lane + 64 * i;
-            if (e < a.E) value[e] = sums ? (z[i] > -INFINITY ? sc[i] : -INFINITY) : unordered(key[i]);
+            for (int i = 0; i < PER; ++i) {
+                const int e = sub + LANES * i;
+                if (e < a.E) value[e] = sums ? (z[i] > -INFINITY ? sc[i] : -INFINITY) : unordered(key[i]);
+            }
         }
+    } else if (a.groups > 1) {
+        float *value = (float *)row + lane / LANES * a.E;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (sub + LANES * i < a.E) value[sub + LANES * i] = z[i];
+    }
+    bool sure = true;   // the same in a token's lanes
+    if (a.groups > 1) {
+        const int lanes = lanes_of_group<LANES>(a.groups);
         wave_lds();
         uint64_t keep;
-        sure = keep_groups<float>(a, value, lanes, lane, !a.bias && !sums, 4 * off, keep);
+        sure = keep_groups<LANES, float>(a, (const float *)row + lane / LANES * a.E, lanes, lane,
+                                         !a.bias && !sums, 4 * off, keep);
         const uint32_t per = a.E / a.groups, inv = ((1u << 20) + per - 1) / per;   // e / per, e < 512
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const uint32_t e = lane + 64 * i;
-            if (!(keep >> ((e * inv >> 20) * lanes) & 1)) key[i] = none;
+            const uint32_t at = ((sub + LANES * i) * inv >> 20) * lanes;
+            if (!(LANES == 16 ? (uint32_t)keep >> at & 1 : (uint32_t)(keep >> at) & 1)) key[i] = none;
         }
     }
-    // lane j: the row's j-th expert and its logit
+    // lane j: the row's j-th expert
     int id = -1;
-    float mine = -INFINITY, before = INFINITY;
+    float before = INFINITY;
     for (int j = 0; j < a.top_k + (a.bias ? 1 : 0); ++j) {
         int m = key[0];
 #pragma unroll
         for (int i = 1; i < PER; ++i) m = max(m, key[i]);
-        m = wave_max(m);
-        if (m <= none) break;
-        if (a.bias) {
+        m = lanes_max<LANES>(m);
+        const bool is = m > none;
+        if (!__any(is)) break;
+        if (a.bias && is) {
             const float v = unordered(m);
             sure = sure && before - v > 2 * off * (1.f + fabsf(v));   // not for infinities
             before = fminf(v, FLT_MAX);
             if (v == INFINITY) sure = false;
         }
-        bool found = false;
+        if constexpr (LANES == 64) {
+            bool found = false;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const uint64_t hit = __ballot(key[i] == m);
-            if (found || !hit) continue;
-            found = true;
-            const int l = __builtin_ctzll(hit);
-            const float zl = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(z[i]), l));
-            if (lane == l) key[i] = none;
-            if (lane == j) id = l + 64 * i, mine = zl;
-        }
-    }
-    if (a.bias && lane >= a.top_k) id = -1, mine = -INFINITY;   // the one looked at for its distance
-    float weight = 0.f;
-    if (!SIGMOID && __any(id >= 0 && mine - top < -690.f)) sure = false;   // scores near 64 bits' end
-    if (sure) {
-        double s = 0.0;
-        if constexpr (SIGMOID) {
-            if (id >= 0) s = 1.0 / (1.0 + exp(-(double)mine));
+            for (int i = 0; i < PER; ++i) {
+                const uint64_t hit = __ballot(key[i] == m);
+                if (found || !hit) continue;
+                found = true;
+                const int l = __builtin_ctzll(hit);
+                if (lane == l) key[i] = none;
+                if (lane == j) id = l + 64 * i;
+            }
         } else {
-            if (id >= 0) s = exp((double)mine - (double)top);
-        }
-        double sum = 1.0;
-        if (a.renormalize) {
-            sum = s;
-            for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-        } else if (!SIGMOID) {
-            sum = 0.0;
+            // the lowest expert with that key: of this lane, then of the token's lanes
+            int mine = kMaxExperts;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) sum += z[i] == -INFINITY ? 0.0 : exp((double)z[i] - (double)top);
-            for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+            for (int i = PER - 1; i >= 0; --i) mine = key[i] == m ? sub + LANES * i : mine;
+            const int e = -lanes_max<LANES>(-mine);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) key[i] = e == sub + LANES * i ? none : key[i];
+            if (sub == j && is) id = e;
         }
-        weight = (float)((sum > 0.0 ? s / sum : 0.0) * (double)a.scale);
-    } else {
-        route_row64<F32, SIGMOID, PER>(a, t, row, lane, id, weight);
     }
-    if (lane < a.top_k) {
-        a.ids[t * a.top_k + lane] = id;
-        a.weights[t * a.top_k + lane] = weight;
+    if (sub >= a.top_k) id = -1;   // the one looked at for its distance
+    const float mine = id >= 0 ? logit(t, id) : -INFINITY;
+    auto any = [&](bool x) {   // in this token's lanes
+        const uint64_t m = __ballot(x) >> (lane & ~(LANES - 1));
+        return LANES == 64 ? m != 0 : (m & ((1ull << (LANES & 63)) - 1)) != 0;
+    };
+    if (!SIGMOID && any(id >= 0 && mine - top < -690.f)) sure = false;   // scores near 64 bits' end
+    double s = 0.0;
+    if constexpr (SIGMOID) {
+        if (id >= 0) s = 1.0 / (1.0 + exp(-(double)mine));
+    } else {
+        if (id >= 0) s = exp((double)mine - (double)top);
+    }
+    double sum = 1.0;
+    if (a.renormalize) {
+        sum = s;
+        for (int o = 1; o < LANES; o <<= 1) sum += __shfl_xor(sum, o);
+    } else if (!SIGMOID) {
+        sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) sum += z[i] == -INFINITY ? 0.0 : exp((double)z[i] - (double)top);
+        for (int o = 1; o < LANES; o <<= 1) sum += __shfl_xor(sum, o);
+    }
+    const float weight = (float)((sum > 0.0 ? s / sum : 0.0) * (double)a.scale);
+    if (sure && sub < a.top_k && t0 + lane / LANES < a.T) {
+        a.ids[t * a.top_k + sub] = id;
+        a.weights[t * a.top_k + sub] = weight;
+    }
+    // the whole wave for each token left
+    for (uint64_t left = __ballot(!sure && sub == 0 && t0 + lane / LANES < a.T); left; left &= left - 1) {
+        const int64_t at = t0 + __builtin_ctzll(left) / LANES;
+        int id64;
+        float w64;
+        wave_lds();
+        route_row64<F32, SIGMOID, (PER * LANES + 63) / 64>(a, at, row, lane, id64, w64);
+        if (lane < a.top_k) {
+            a.ids[at * a.top_k + lane] = id64;
+            a.weights[at * a.top_k + lane] = w64;
+        }
     }
 }
 
+template <bool F32, bool SIGMOID, int LANES>
+void launch_route(const RouteArgs &a, hipStream_t st) {
+    constexpr int U = 64 / LANES;
+    const dim3 grid((unsigned)cdiv(a.T, 4 * U)), block(256);
+    const size_t lds = a.groups > 1 ? 4 * (size_t)a.E * std::max(8, 4 * U) : 0;
+    if (a.E <= 64) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, U, LANES>), grid, block, lds, st, a);
+    else if (a.E <= 128) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 2 * U, LANES>), grid, block, lds, st, a);
+    else if (a.E <= 256) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 4 * U, LANES>), grid, block, lds, st, a);
+    else hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 8 * U, LANES>), grid, block, lds, st, a);
+}
+
+// Sixteen lanes a token take half the instructions, but four times as long over one
+// token: many tokens go that way, where 16 lanes have a place for each chosen expert
+// and the next, and one for each group (wave a token, then 16 lanes: 2,000 tokens of
+// 256 experts 8.5 and 11.3 us, 8,000 24.4 and 21.3; of 64 experts 2,000 4.3 and 4.5,
+// 8,000 6.8 and 4.7; of 512 experts 2,000 8.3 and 12.0, 8,000 16.8 and 14.4).
 template <bool F32, bool SIGMOID>
 void launch_route(const RouteArgs &a, hipStream_t st) {
-    const dim3 grid((unsigned)cdiv(a.T, 4)), block(256);
-    const size_t lds = a.groups > 1 ? 4 * a.E * sizeof(double) : 0;
-    if (a.E <= 64) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 1>), grid, block, lds, st, a);
-    else if (a.E <= 128) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 2>), grid, block, lds, st, a);
-    else if (a.E <= 256) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 4>), grid, block, lds, st, a);
-    else hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 8>), grid, block, lds, st, a);
+    if (a.T > 4096 && a.top_k < 16 && a.groups <= 16) launch_route<F32, SIGMOID, 16>(a, st);
+    else launch_route<F32, SIGMOID, 64>(a, st);
 }
 
 // ------------------------------------------------------------ the experts

@@ -87,6 +87,33 @@ def test_route_keys_closer_than_fp32_tells(score, kw):
     _same_route(_route(z, kw, b), FO.route(z, bias=b, **kw))
 
 
+@pytest.mark.parametrize("bias", [False, True, "equal"])
+@pytest.mark.parametrize("E, kw", [
+    (1, dict(top_k=1)), (8, dict(top_k=2, renormalize=True)), (60, dict(top_k=15)),
+    (130, dict(top_k=4, num_groups=13, top_groups=3, group_top=2, renormalize=True)),
+    (160, dict(top_k=6, num_groups=16, top_groups=5)),
+    (256, dict(top_k=8, num_groups=8, top_groups=4, group_top=2)),
+    (512, dict(top_k=15, num_groups=2, top_groups=2, group_top=2, renormalize=True))])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_route_many_tokens(E, kw, score, bias):
+    """Rows of random logits, masked ones among them, ties, and (bias "equal") rows whose
+    keys are closer than fp32 tells, over and over in a batch of 4,101 tokens."""
+    g = np.random.default_rng(E)
+    z = (2 * g.standard_normal((37, E))).astype(np.float32)
+    z[3], z[7, ::2], z[8, E // 3:], z[9] = -np.inf, -np.inf, np.nan, np.round(z[9])
+    z[20:30] = z[20]
+    z[21:30] += (g.integers(-2, 3, (9, E)) * np.float32(2.0 ** -23)).astype(np.float32)
+    b = (0.3 * g.standard_normal(E)).astype(np.float32) if bias else None
+    if bias == "equal":
+        z64 = z[20].astype(np.float64)
+        s = np.exp(z64) / np.exp(z64).sum() if score == "softmax" else 1 / (1 + np.exp(-z64))
+        b = (0.75 - s).astype(np.float32)
+    kw = dict(kw, score=score)
+    ids, w = FO.route(z, bias=b, **kw)
+    at = np.arange(4101) % 37
+    _same_route(_route(z[at], kw, b, pad=3), (ids[at], w[at]))
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("groups", [1, 4])
 @pytest.mark.parametrize("group_top", [1, 2])
@@ -124,6 +151,8 @@ def test_route_ties_masks_and_extremes(score, groups, group_top, bias):
         kw.update(renormalize=False, scale=-0.5)
     got, want = _route(z, kw, b), FO.route(z, bias=b, **kw)
     _same_route(got, want)
+    many = np.arange(4100) % 16
+    _same_route(_route(z[many], kw, b), (want[0][many], want[1][many]))
     assert (got[0][1:3] == -1).all() and (got[1][1:3] == 0).all()
 
 
