@@ -80,87 +80,106 @@ __device__ __forceinline__ int lanes_of_group(int groups) {
     return l;
 }
 
+__device__ __forceinline__ float read_logit(const void *logits, bool f32, int64_t at) {
+    const float f = f32 ? ((const float *)logits)[at] : bf2f(((const uint16_t *)logits)[at]);
+    return f > -INFINITY ? fminf(f, FLT_MAX) + 0.f : -INFINITY;   // NaN too; -0 becomes 0
+}
+
+// fp64 as integers of the same order (no NaN; -0 and 0 made equal first), and their
+// max over the wave: rotations in rows of 16 lanes, then swaps of rows and halves
+__device__ __forceinline__ int64_t ordered64(double x) {
+    const int64_t b = __double_as_longlong(x);
+    return b ^ ((b >> 63) & INT64_MAX);
+}
+__device__ __forceinline__ int64_t two_words(uint32_t lo, uint32_t hi) { return (int64_t)((uint64_t)hi << 32 | lo); }
+template <int DPP>
+__device__ __forceinline__ int64_t max_of_turn(int64_t v) {
+    return max(v, two_words(__builtin_amdgcn_update_dpp(0, (uint32_t)v, DPP, 0xF, 0xF, false),
+                            __builtin_amdgcn_update_dpp(0, (uint32_t)(v >> 32), DPP, 0xF, 0xF, false)));
+}
+__device__ __forceinline__ int64_t wave_max64(int64_t v) {
+    v = max_of_turn<0x121>(max_of_turn<0x122>(max_of_turn<0x124>(max_of_turn<0x128>(v))));   // row_ror
+    const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    const auto b = __builtin_amdgcn_permlane16_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
+    v = max(two_words(a[0], b[0]), two_words(a[1], b[1]));
+    const auto c = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    const auto d = __builtin_amdgcn_permlane32_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
+    return max(two_words(c[0], d[0]), two_words(c[1], d[1]));
+}
+
 // The definition, in 64 bits: what route_kernel takes where 32 do not decide.
-// id and weight of lane j: of the row's j-th expert.
+// id and weight of lane j: of the row's j-th expert.  `row`: E doubles of LDS.
+// Few rows come here and each waits for its instructions: loops stay loops.
 template <bool F32, bool SIGMOID, int PER>
 __device__ __forceinline__ void route_row64(const RouteArgs &a, int64_t t, double *row, int lane,
                                             int &id, float &weight) {
-    double score[PER], key[PER];
-    double top = -DBL_MAX;
+    auto logit = [&](int e) { return (double)read_logit(a.logits, F32, t * a.stride + e); };
+    double top = -DBL_MAX, sum = 0.0;   // softmax: the largest logit, and the sum
+    if constexpr (!SIGMOID) {
+#pragma unroll 1
+        for (int e = lane; e < a.E; e += 64) top = fmax(top, logit(e));
+        for (int o = 1; o < 64; o <<= 1) top = fmax(top, __shfl_xor(top, o));
+#pragma unroll 1
+        for (int e = lane; e < a.E; e += 64) {
+            const double z = logit(e);
+            sum += z == -INFINITY ? 0.0 : exp(z - top);
+        }
+        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    }
+    auto score = [&](double z) {
+        if constexpr (SIGMOID) return z == -INFINITY ? 0.0 : 1.0 / (1.0 + exp(-z));
+        else return z == -INFINITY || !(sum > 0.0) ? 0.0 : exp(z - top) / sum;
+    };
+    // keys, or what groups go by: a sum of two is of scores
+    const bool scores = a.bias || (a.groups > 1 && a.group_top == 2);
+#pragma unroll 1
+    for (int e = lane; e < a.E; e += 64) {
+        const double z = logit(e);
+        double k = z;
+        if (scores && z > -INFINITY) {
+            k = score(z);
+            if (a.bias) k += (double)a.bias[e];
+            k = k > -INFINITY ? fmin(k, DBL_MAX) : -INFINITY;   // a NaN too
+        }
+        row[e] = k;
+    }
+    wave_lds();
+    uint64_t keep = ~0ull;
+    const int per = a.E / a.groups, lanes = lanes_of_group<64>(a.groups);
+    if (a.groups > 1) keep_groups<64, double>(a, row, lanes, lane, true, 0.0, keep);
+    int64_t key[PER];
+    const int64_t none = ordered64(-INFINITY);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int e = lane + 64 * i;
-        double z = -INFINITY;
-        if (e < a.E) {
-            const int64_t at = t * a.stride + e;
-            const float f = F32 ? ((const float *)a.logits)[at] : bf2f(((const uint16_t *)a.logits)[at]);
-            if (f > -INFINITY) z = fmin((double)f, (double)FLT_MAX);   // not for NaN
-        }
-        key[i] = z;
-        top = fmax(top, z);
+        key[i] = none;
+        if (e < a.E && (keep >> (e / per * lanes) & 1)) key[i] = ordered64((a.bias ? row[e] : logit(e)) + 0.0);
     }
-    if constexpr (SIGMOID) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) score[i] = key[i] == -INFINITY ? 0.0 : 1.0 / (1.0 + exp(-key[i]));
-    } else {
-        for (int o = 1; o < 64; o <<= 1) top = fmax(top, __shfl_xor(top, o));
-        double sum = 0.0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            score[i] = key[i] == -INFINITY ? 0.0 : exp(key[i] - top);
-            sum += score[i];
-        }
-        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) score[i] = sum > 0.0 ? score[i] / sum : 0.0;
-    }
-    if (a.bias) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = lane + 64 * i;
-            double k = key[i] == -INFINITY ? -INFINITY : score[i] + (double)a.bias[min(e, a.E - 1)];
-            if (!(k > -INFINITY)) k = -INFINITY;   // a NaN too
-            key[i] = fmin(k, DBL_MAX);
-        }
-    }
-    if (a.groups > 1) {
-        const int per = a.E / a.groups, lanes = lanes_of_group<64>(a.groups);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = lane + 64 * i;
-            // a sum of two is of scores
-            if (e < a.E) row[e] = a.group_top == 2 && !a.bias && key[i] > -INFINITY ? score[i] : key[i];
-        }
-        wave_lds();
-        uint64_t keep;
-        keep_groups<64, double>(a, row, lanes, lane, true, 0.0, keep);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = lane + 64 * i;
-            if (e < a.E && !(keep >> (e / per * lanes) & 1)) key[i] = -INFINITY;
-        }
-    }
-    double mine = 0.0, sum = 0.0;   // lane j: the score of the row's j-th expert
     id = -1;
+#pragma unroll 1
     for (int j = 0; j < a.top_k; ++j) {
-        double v = -INFINITY, sc = 0.0;
-        int at = 0x7FFFFFFF;
+        int64_t m = key[0];
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (key[i] > v) v = key[i], at = lane + 64 * i, sc = score[i];
-        for (int o = 1; o < 64; o <<= 1) {
-            const double ov = __shfl_xor(v, o), os = __shfl_xor(sc, o);
-            const int oa = __shfl_xor(at, o);
-            if (ahead(ov, oa, v, at)) v = ov, at = oa, sc = os;
+        for (int i = 1; i < PER; ++i) m = max(m, key[i]);
+        m = wave_max64(m);
+        if (m <= none) break;
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint64_t hit = __ballot(key[i] == m);
+            if (found || !hit) continue;
+            found = true;
+            const int l = __builtin_ctzll(hit);
+            if (lane == l) key[i] = none;
+            if (lane == j) id = l + 64 * i;
         }
-        if (v == -INFINITY) break;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (at == lane + 64 * i) key[i] = -INFINITY;
-        if (lane == j) id = at, mine = sc;
-        sum += sc;
     }
-    const double w = a.renormalize ? (sum > 0.0 ? mine / sum : 0.0) : mine;
+    double w = id >= 0 ? score(logit(id)) : 0.0;
+    if (a.renormalize) {
+        double all = w;
+        for (int o = 1; o < 64; o <<= 1) all += __shfl_xor(all, o);
+        w = all > 0.0 ? w / all : 0.0;
+    }
     weight = (float)(w * (double)a.scale);
 }
 
@@ -195,9 +214,9 @@ __device__ __forceinline__ int lanes_max(int v) {
 // reciprocal's), below 2^-19.  Where two neighbours among the chosen and the next,
 // or the groups at the border, are not further apart than that the row goes to
 // route_row64.  The chosen experts' scores are taken in 64 bits.
-// Bound by instructions, and where rows go to route_row64 by its 8 us: 16,412 tokens
-// of 256 experts, 8 chosen of 4 groups of 8 with a bias, take 27 us (34 with a wave
-// a token).
+// Bound by instructions, and where rows go to route_row64 by its 5.5 us: 16,412
+// tokens of 256 experts, 8 chosen of 4 groups of 8 with a bias, take 25 us (34 with a
+// wave a token, 60 all in 64 bits).
 template <bool F32, bool SIGMOID, int PER, int LANES>
 __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
     extern __shared__ double route_lds[];
@@ -210,15 +229,11 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
     const int64_t t = min(t0 + lane / LANES, (int64_t)a.T - 1);
     constexpr float off = SIGMOID ? 0x1p-21f : 0x1p-19f;
     // of a wave: E doubles, or E floats of each token
-    double *row = route_lds + wave * (a.groups > 1 ? a.E * (TOKENS > 1 ? TOKENS / 2 : 1) : 0);
+    double *row = route_lds + wave * a.E * (TOKENS > 1 ? TOKENS / 2 : 1);
     float z[PER];
     int key[PER];
     const int none = ordered(-INFINITY);
-    auto logit = [&](int64_t t, int e) {
-        const int64_t at = t * a.stride + e;
-        const float f = F32 ? ((const float *)a.logits)[at] : bf2f(((const uint16_t *)a.logits)[at]);
-        return f > -INFINITY ? fminf(f, FLT_MAX) + 0.f : -INFINITY;   // NaN too; -0 becomes 0
-    };
+    auto logit = [&](int64_t t, int e) { return read_logit(a.logits, F32, t * a.stride + e); };
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int e = sub + LANES * i;
@@ -370,7 +385,7 @@ template <bool F32, bool SIGMOID, int LANES>
 void launch_route(const RouteArgs &a, hipStream_t st) {
     constexpr int U = 64 / LANES;
     const dim3 grid((unsigned)cdiv(a.T, 4 * U)), block(256);
-    const size_t lds = a.groups > 1 ? 4 * (size_t)a.E * std::max(8, 4 * U) : 0;
+    const size_t lds = 4 * (size_t)a.E * std::max(8, 4 * U);
     if (a.E <= 64) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, U, LANES>), grid, block, lds, st, a);
     else if (a.E <= 128) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 2 * U, LANES>), grid, block, lds, st, a);
     else if (a.E <= 256) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 4 * U, LANES>), grid, block, lds, st, a);
@@ -379,9 +394,9 @@ void launch_route(const RouteArgs &a, hipStream_t st) {
 
 // Sixteen lanes a token take half the instructions, but four times as long over one
 // token: many tokens go that way, where 16 lanes have a place for each chosen expert
-// and the next, and one for each group (wave a token, then 16 lanes: 2,000 tokens of
-// 256 experts 8.5 and 11.3 us, 8,000 24.4 and 21.3; of 64 experts 2,000 4.3 and 4.5,
-// 8,000 6.8 and 4.7; of 512 experts 2,000 8.3 and 12.0, 8,000 16.8 and 14.4).
+// and the next, and one for each group (a wave a token, then 16 lanes: 2,000 tokens
+// of 512 experts 8.3 and 12.0 us, 8,000 16.8 and 14.4; of 64 experts 2,000 4.3 and
+// 4.5, 8,000 6.8 and 4.7).
 template <bool F32, bool SIGMOID>
 void launch_route(const RouteArgs &a, hipStream_t st) {
     if (a.T > 4096 && a.top_k < 16 && a.groups <= 16) launch_route<F32, SIGMOID, 16>(a, st);
