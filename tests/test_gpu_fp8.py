@@ -219,6 +219,47 @@ def test_gemm_on_another_stream_and_replayed(T):
         assert torch.equal(y.view(torch.int16), eager.view(torch.int16)), r
 
 
+@pytest.mark.parametrize("T, N, K", [(20, 70001, 144), (50, 66000, 272), (100, 34008, 272),
+                                     (200, 34000, 144), (700, 17000, 272), (1500, 12000, 400)])
+def test_gemm_of_more_tiles_than_run_at_once(T, N, K):
+    """Workgroups go from tile to tile: edges in both directions, a whole residual."""
+    g = np.random.default_rng(T)
+    x, xs = activations(g, T, K)
+    w, ws = weights(g, N, K)
+    say(f"[case] gemm T={T} N={N} K={K}")
+    r = bf16_round(g.standard_normal((T, N)).astype(np.float32)) if T % 200 == 100 else None
+    want, S = FO.gemm(x, xs, w, ws) if r is None else FO.gemm(x, xs, w, ws, r)
+    _check(_gemm(x, xs, w, ws, False, r), want, S if r is None else S + np.abs(r), K, False)
+    if T < 150:
+        want, S = FO.gemm(x, xs, w, ws)
+        _check(_gemm(x, xs, w, ws, True), want, S, K, True)
+
+
+def test_tokens_past_32_bits():
+    """More than 2^32 values quantised and codes multiplied: the first and last rows."""
+    import torch
+    from paper_2504_03651_amd import fp8
+    g = np.random.default_rng(8)
+    T, K = 262144 + 40, 16400
+    a = bf16_round(g.standard_normal((2, 100, K)).astype(np.float32))
+    x = torch.zeros(T, K, dtype=torch.bfloat16, device="cuda")
+    x[:100], x[-100:] = dev(a[0]), dev(a[1])
+    codes = torch.full((T, K), 0x55, dtype=torch.uint8, device="cuda")
+    scales = torch.zeros(T, fp8.blocks(K), device="cuda")
+    fp8.quantize(x, codes, scales)
+    w, ws = weights(g, 40, K)
+    y = torch.empty(T, 40, dtype=torch.bfloat16, device="cuda")
+    n = fp8.gemm_workspace_bytes(T, 40, K)
+    fp8.gemm(codes, scales, dev(w), dev(ws), y,
+             workspace=torch.empty(n, dtype=torch.uint8, device="cuda") if n else None)
+    for i, at in enumerate((slice(0, 100), slice(T - 100, T))):
+        c, s = FO.quantize(a[i], 1)
+        assert np.array_equal(codes[at].cpu().numpy(), c) and np.array_equal(scales[at].cpu().numpy(), s)
+        want, S = FO.gemm(c, s, w, ws)
+        _check(y[at].double().cpu().numpy(), want, S, K, False)
+    assert (codes[100:-100] == 0).all() and (y[100:-100] == 0).all()
+
+
 def test_gemm_offsets_past_32_bits():
     """Weights of more than 2^32 codes and outputs past 2^32 bytes: the last rows."""
     import torch

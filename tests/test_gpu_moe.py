@@ -201,7 +201,9 @@ def _routing(g, T, E, k, skew=1.0):
 @pytest.mark.parametrize("T, E, k, H, I", [
     (1, 1, 1, 16, 16), (1, 8, 2, 256, 128), (3, 4, 2, 144, 272), (7, 64, 8, 256, 144), (20, 3, 3, 400, 112),
     (64, 16, 2, 512, 256), (129, 8, 2, 272, 400), (300, 5, 2, 256, 384), (257, 2, 1, 1040, 128),
-    (500, 4, 4, 128, 640), (40, 512, 4, 128, 48), (1000, 16, 4, 384, 256)])
+    (500, 4, 4, 128, 640), (40, 512, 4, 128, 48), (1000, 16, 4, 384, 256),
+    # more tiles than run at once, of 16, 32, 64 and 128 pairs
+    (300, 512, 4, 256, 400), (701, 512, 4, 272, 400), (401, 200, 8, 512, 400), (501, 40, 8, 1536, 1040)])
 def test_experts(T, E, k, H, I):
     g = np.random.default_rng(T + E + H)
     host = experts_weights(g, E, H, I)
