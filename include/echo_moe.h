@@ -69,8 +69,9 @@ typedef struct {
  * [T][top_k], residual (optional; may be out itself) and out bf16 [T][H].
  * Inside an expert the activation SiLU(gate) * up, in fp32, is requantised in
  * blocks of 1 x 128 as echo_fp8_quantize does (quotients within two ulps); an
- * expert's output is rounded to bf16 before the weighted sum, which is taken
- * in fp32 in the order of j.  A pair whose id lies outside [0, E)
+ * expert's output is rounded to 11 bits (2^-11 of the value, or 2^-39 of the
+ * largest of its 16 or more neighbours) before the weighted sum, which is taken in
+ * fp32 in the order of j.  A pair whose id lies outside [0, E)
  * adds nothing, whatever its weight: padding, or experts held elsewhere.  An
  * expert may stand twice in a row.  T * top_k at most 2^24; top_k 1..64; T * H
  * and 2 I H below 2^32.

@@ -117,7 +117,8 @@ def route(logits, top_k, score="softmax", num_groups=1, top_groups=1, group_top=
 def experts(x, xs, ids, weights, w_gate_up, gate_up_scale, w_down, down_scale, residual=None):
     """(out, bound) in fp64: bound is how far a result may be off besides its own
     rounding, for an e4m3 step (2^-3 of the value at most) of single activation
-    codes next to a border, and the rounding of an expert's output to bf16."""
+    codes next to a border, and the rounding of an expert's output to 11 bits under
+    the largest of its neighbours (here of its row)."""
     E, H, I = w_down.shape
     T = x.shape[0]
     a = values(x, xs, 1)
@@ -142,5 +143,6 @@ def experts(x, xs, ids, weights, w_gate_up, gate_up_scale, w_down, down_scale, r
         y = h @ d.T
         wt = np.asarray(weights, np.float64)[t, j][:, None]
         np.add.at(out, t, wt * y)
-        np.add.at(bound, t, np.abs(wt) * (2.0 ** -8 * np.abs(y) + 2.0 ** -3 * np.sqrt((h * h) @ (d * d).T)))
+        off = 2.0 ** -11 * np.abs(y) + 2.0 ** -39 * np.abs(y).max(1, keepdims=True)
+        np.add.at(bound, t, np.abs(wt) * (off + 2.0 ** -3 * np.sqrt((h * h) @ (d * d).T)))
     return out, bound

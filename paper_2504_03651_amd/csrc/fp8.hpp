@@ -28,6 +28,13 @@ __device__ __forceinline__ uint32_t f2bf2(float x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x, y}, bf16x2));
 }
 
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// Two fp32 -> two fp16, round to nearest even
+__device__ __forceinline__ uint32_t f2h2(float x, float y) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x, y}, f16x2));
+}
+
 // Two fp32 -> two e4m3fn codes in the low 16 bits, round to nearest even,
 // saturating at 448, NaN to 0x7F (v_cvt_pk_fp8_f32 on clamped values).
 __device__ __forceinline__ uint32_t e4m3x2(float x, float y) {
@@ -89,7 +96,8 @@ __device__ __forceinline__ i32x8 pair(u32x4 lo, u32x4 hi) {
 //   GateUp  rows are (token, expert) pairs in order of expert; a tile's pair p
 //           reads token order[p] / top_k and writes codes and scales of row p of
 //           SiLU(x . w[n]) * (x . w[N + n]), n < N = I
-//   Down    pair p reads row p and writes row order[p] of y
+//   Down    pair p reads row p and writes row order[p] of y, fp16 times powers of
+//           two whose exponents, of groups of a wave's columns, go to ye
 enum class Mode { Plain, GateUp, Down };
 
 struct Tile {
@@ -119,6 +127,9 @@ struct ProductArgs {
     const Tile *tiles;
     const int *order;      // pair of each place
     int top_k;
+    // Down
+    int8_t *ye;            // [pairs][y_groups]
+    int y_groups;
 };
 
 // LDS written by lanes of this wave is there for its other lanes

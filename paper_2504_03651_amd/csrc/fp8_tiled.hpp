@@ -25,6 +25,9 @@ __device__ __forceinline__ void landed_but() {
 // through LDS, so that a store instruction writes whole pieces of rows: the tile
 // has them by columns, four values of a row a lane.
 // Uses at most ROOM bytes of LDS, in PASSES where the whole tile needs more.
+// An expert's outputs (Down) keep 11 bits in fp16 under an exponent of their own for
+// each row's NW columns: no more than 2^-11 of the value off, or 2^-39 of the
+// largest of those columns, at half the bytes of fp32.
 template <Mode M, bool F32, int BN, int BT, int WN, int WT, int ROOM>
 __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
                                        f32x4 (&acc)[BN / WN / 16][BT / WT / 16], int n_tiles, int nb,
@@ -129,6 +132,22 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
             for (int j = 0; j < TP / 16; ++j) {
                 const int r = 16 * j + c;
                 const bool live = t0 + r < rows;
+                int up = 0;
+                if constexpr (M == Mode::Down) {
+                    float m = 0.f;
+#pragma unroll
+                    for (int i = 0; i < NI; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float a = fabsf(acc[i][pass * (TP / 16) + j][e]);
+                            m = fmaxf(m, a < INFINITY ? a : 0.f);   // not a NaN either
+                        }
+                    m = fmaxf(m, __shfl_xor(m, 16));
+                    m = fmaxf(m, __shfl_xor(m, 32));
+                    up = min(15 - __builtin_amdgcn_frexp_expf(m), 127);   // m 2^up below 2^15
+                    if (live && g == 0 && n0 + wn * NW < p.N)
+                        p.ye[p.order[row0 + t0 + r] * (int64_t)p.y_groups + (n0 + wn * NW) / NW] = (int8_t)-up;
+                }
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
                     f32x4 v = acc[i][pass * (TP / 16) + j];
@@ -139,8 +158,15 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
 #pragma unroll
                         for (int e = 0; e < 2; ++e) v[2 * e] += bf2f(q[e] & 0xFFFFu), v[2 * e + 1] += bf2f(q[e] >> 16);
                     }
-                    *(u32x2 *)(mine + (r * Q + ((n >> 3) ^ (r & (Q - 1)))) * 16 + (n & 4) * 2) =
-                        (u32x2){f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+                    u32x2 two;
+                    if constexpr (M == Mode::Down) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_ldexpf(v[e], up);
+                        two = (u32x2){f2h2(v[0], v[1]), f2h2(v[2], v[3])};
+                    } else {
+                        two = (u32x2){f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+                    }
+                    *(u32x2 *)(mine + (r * Q + ((n >> 3) ^ (r & (Q - 1)))) * 16 + (n & 4) * 2) = two;
                 }
             }
             wave_lds();

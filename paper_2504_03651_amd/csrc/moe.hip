@@ -492,26 +492,29 @@ __global__ __launch_bounds__(1024) void place_pairs_kernel(const int32_t *ids, i
     }
 }
 
-// out[t] = residual[t] + sum_j weights[t][j] y[t][j], eight columns a thread
-__global__ __launch_bounds__(256) void combine_kernel(const uint16_t *y, const int32_t *ids,
-                                                      const float *weights, const uint16_t *residual,
-                                                      uint16_t *out, int64_t n8, int H, int E,
-                                                      int top_k) {
+// out[t] = residual[t] + sum_j weights[t][j] y[t][j], eight columns a thread; y fp16
+// times 2^ye, of 2^shift columns each
+__global__ __launch_bounds__(256) void combine_kernel(const uint16_t *y, const int8_t *ye, int shift,
+                                                      const int32_t *ids, const float *weights,
+                                                      const uint16_t *residual, uint16_t *out,
+                                                      int64_t n8, int H, int E, int top_k) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= n8) return;
     const int64_t t = i / (H / 8);
-    const int h = 8 * (int)(i - t * (H / 8));
+    const int h = 8 * (int)(i - t * (H / 8)), groups = ((H - 1) >> shift) + 1;
     float v[8] = {};
     for (int j = 0; j < top_k; ++j) {
         const int64_t pair = t * top_k + j;
         const int e = ids[pair];
         if (e < 0 || e >= E) continue;
         const float w = weights[pair];
+        const int up = ye[pair * groups + (h >> shift)];
         const u32x4 q = *(const u32x4 *)(y + pair * H + h);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            v[2 * r] += w * bf2f(q[r] & 0xFFFFu);
-            v[2 * r + 1] += w * bf2f(q[r] >> 16);
+            const f16x2 two = __builtin_bit_cast(f16x2, (uint32_t)q[r]);
+            v[2 * r] += w * __builtin_amdgcn_ldexpf((float)two[0], up);
+            v[2 * r + 1] += w * __builtin_amdgcn_ldexpf((float)two[1], up);
         }
     }
     if (residual) {
@@ -536,7 +539,7 @@ namespace {
 struct Ws {
     int tile, max_tiles;   // rows of a tile, and the most tiles there can be
     int chunk, chunks;     // pairs that a workgroup places, and workgroups
-    size_t num_tiles, counts, tiles, order, hs, hc, y, total;
+    size_t num_tiles, counts, tiles, order, hs, hc, y, ye, total;
 };
 
 int plan_ws(const echo_experts_t *x, int32_t T, int32_t top_k, Ws *w) {
@@ -577,6 +580,7 @@ int plan_ws(const echo_experts_t *x, int32_t T, int32_t top_k, Ws *w) {
     w->hs = take(4 * R * cdiv(x->intermediate, kQ));
     w->hc = take(R * x->intermediate);
     w->y = take(2 * R * x->hidden);
+    w->ye = take(R * cdiv(x->hidden, 16));   // of 16 columns or more
     w->total = R ? o : 0;
     return ECHO_OK;
 }
@@ -587,12 +591,14 @@ int launched(const char *what) {
 }
 
 // The forms of both products: the gate and up rows of 128 columns, and rows of
-// the down matrix, by the tile's pairs.
+// the down matrix, by the tile's pairs.  columns: of y under one exponent.
 template <int BT, int GN, int GT, int GS, int BN, int DN, int DT, int DS>
-hipError_t run_experts(const ProductArgs &gu, const ProductArgs &dn, int max_tiles, hipStream_t st) {
+hipError_t run_experts(const ProductArgs &gu, ProductArgs dn, int max_tiles, int *columns, hipStream_t st) {
     hipError_t e = launch_tiled<Mode::GateUp, false, (BT <= 64), 256, BT, GN, GT, GS>(gu, max_tiles, 1, st);
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess) return e;
+    *columns = BN / DN;
+    dn.y_groups = cdiv(dn.N, *columns);
     return launch_tiled<Mode::Down, false, (BT <= 64), BN, BT, DN, DT, DS>(dn, max_tiles, 1, st);
 }
 
@@ -716,16 +722,19 @@ int echo_moe_experts(const echo_experts_t *m, const void *x, const float *x_scal
     dn.y = base + w.y;
     dn.y_stride = H;
     dn.wide = dn.pieces = true;   // H a multiple of 16, y the workspace's
-    const hipError_t e = w.tile == 128  ? run_experts<128, 4, 2, 3, 256, 4, 2, 3>(gu, dn, w.max_tiles, st)
-                         : w.tile == 64 ? run_experts<64, 4, 2, 3, 128, 4, 1, 3>(gu, dn, w.max_tiles, st)
-                         : w.tile == 32 ? run_experts<32, 4, 1, 2, 128, 4, 1, 3>(gu, dn, w.max_tiles, st)
-                                        : run_experts<16, 8, 1, 2, 64, 4, 1, 4>(gu, dn, w.max_tiles, st);
+    dn.ye = (int8_t *)(base + w.ye);
+    int columns = 0;
+    const hipError_t e =
+        w.tile == 128  ? run_experts<128, 4, 2, 3, 256, 4, 2, 3>(gu, dn, w.max_tiles, &columns, st)
+        : w.tile == 64 ? run_experts<64, 4, 2, 3, 128, 4, 1, 3>(gu, dn, w.max_tiles, &columns, st)
+        : w.tile == 32 ? run_experts<32, 4, 1, 2, 128, 4, 1, 3>(gu, dn, w.max_tiles, &columns, st)
+                       : run_experts<16, 8, 1, 2, 64, 4, 1, 4>(gu, dn, w.max_tiles, &columns, st);
     if (e != hipSuccess) return fail(ECHO_E_HIP, "experts' products: %s", hipGetErrorString(e));
     if ((rc = launched("experts' products"))) return rc;
     const int64_t n8 = (int64_t)num_tokens * H / 8;
     if (n8 > 256 * (int64_t)INT32_MAX) return fail(ECHO_E_UNSUPPORTED, "output too large");
     hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((n8 + 255) / 256)), dim3(256), 0, st,
-                       (const uint16_t *)(base + w.y), ids, weights, (const uint16_t *)residual,
+                       (const uint16_t *)(base + w.y), dn.ye, __builtin_ctz(columns), ids, weights, (const uint16_t *)residual,
                        (uint16_t *)out, n8, H, E, top_k);
     return launched("weighted sum");
 }

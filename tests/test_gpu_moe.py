@@ -3,7 +3,7 @@
 The chosen experts are compared exactly and the weights to a rounding of fp32
 (2^-24 relative, and 1e-13 for the 64-bit scores).  An experts' output may be off by
 a half step of bf16 (2^-8 relative) and what the reference allows for expert
-outputs rounded to bf16 and activation codes next to a border
+outputs rounded to 11 bits and activation codes next to a border
 (oracle/fp8_oracle.py); the error's 2-norm stays below 2^-7 of the result's.
 """
 import numpy as np
@@ -242,6 +242,27 @@ def test_experts_padding_repeats_and_foreign_ids(T):
     _near(_experts(host, ids, wt, x, xs), want, bound)
     ids[:] = -1
     assert (_experts(host, ids, wt, x, xs) == 0).all()
+
+
+@pytest.mark.parametrize("T", [3, 50, 100, 700])
+def test_experts_outputs_of_any_magnitude(T):
+    """Columns under scales as far apart as fp32 goes, each block of them against its
+    own reference; one expert's outputs are zero, and two tokens' inputs."""
+    g = np.random.default_rng(T)
+    E, k, H, I = 3, 2, 400, 144
+    host = experts_weights(g, E, H, I)
+    for b, m in enumerate((2.0 ** -118, 1.0, 2.0 ** 96, 2.0 ** -60)):
+        host[3][:, b] *= np.float32(m)
+    host[3][1] = 0
+    x, xs = activations(g, T, H)
+    x[:2] = 0
+    ids, wt = _routing(g, T, E, k)
+    got = _experts(host, ids, wt, x, xs)
+    for b in range(4):
+        at = slice(128 * b, min(128 * b + 128, H))
+        want, bound = FO.experts(x, xs, ids, wt, host[0], host[1], host[2][:, at], host[3][:, b:b + 1])
+        _near(got[:, at], want, bound)
+    assert (got[:2] == 0).all()
 
 
 def test_experts_nan_stays_in_its_token():
