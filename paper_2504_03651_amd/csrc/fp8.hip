@@ -430,8 +430,6 @@ int echo_fp8_gemm(const void *x, const float *x_scale, const void *w, const floa
     p.y_stride = y_stride;
     p.part = (float *)workspace;
     p.part_pitch = pitch_of(out_features);
-    p.wide = out_features % 4 == 0 && y_stride % 4 == 0 && !(ya & (y_dtype == ECHO_F32 ? 15u : 7u));
-    p.pieces = y_dtype == ECHO_BF16 && out_features % 8 == 0 && y_stride % 8 == 0 && !((uintptr_t)y & 15u) && p.wide;
     const hipError_t e = y_dtype == ECHO_F32 ? launch_gemm<true>(p, cut, (hipStream_t)stream)
                                              : launch_gemm<false>(p, cut, (hipStream_t)stream);
     if (e != hipSuccess) return fail(ECHO_E_HIP, "echo_fp8_gemm: %s", hipGetErrorString(e));

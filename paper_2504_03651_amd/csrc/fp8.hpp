@@ -115,8 +115,6 @@ struct ProductArgs {
     const void *residual;
     void *y;
     int64_t y_stride;
-    bool wide;             // see store4
-    bool pieces;           // wide, with rows of y at 16-byte steps and N a multiple of 8
     float *part;           // [splits][T][part_pitch], for products over ranges of K
     int part_pitch;
     // GateUp
@@ -138,37 +136,59 @@ __device__ __forceinline__ void wave_lds() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// y of a lane's four columns n .. n + 3 of row t, the residual added; p.wide:
-// N and y_stride multiples of 4, y and residual aligned to four values
+// Memory that need not be aligned to more than its elements: the hardware takes such
+// accesses of 8 and 16 bytes, which the compiler emits for these types.
+typedef u32x4 __attribute__((aligned(2))) any_u32x4;
+typedef u32x2 __attribute__((aligned(2))) any_u32x2;
+typedef f32x4 __attribute__((aligned(4))) any_f32x4;
+
+// v plus the residual of a lane's four columns n .. n + 3 at element `at`
+template <bool F32>
+__device__ __forceinline__ f32x4 plus_residual(const ProductArgs &p, int64_t at, int n, f32x4 v) {
+    if constexpr (F32) {
+        const float *r = (const float *)p.residual + at;
+        if (n + 4 <= p.N) return v + *(const any_f32x4 *)r;
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (n + e < p.N) v[e] += r[e];
+    } else {
+        const uint16_t *r = (const uint16_t *)p.residual + at;
+        if (n + 4 <= p.N) {
+            const u32x2 q = *(const any_u32x2 *)r;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) v[2 * e] += bf2f(q[e] & 0xFFFFu), v[2 * e + 1] += bf2f(q[e] >> 16);
+            return v;
+        }
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (n + e < p.N) v[e] += bf2f(r[e]);
+    }
+    return v;
+}
+
+// y of a lane's four columns n .. n + 3 of row t, the residual added
 template <bool F32>
 __device__ __forceinline__ void store4(const ProductArgs &p, int64_t t, int n, f32x4 v) {
     const int64_t at = t * p.y_stride + n;
-    if (p.wide) {
-        if (n >= p.N) return;
-        if constexpr (F32) {
-            if (p.residual) v += *(const f32x4 *)((const float *)p.residual + at);
-            *(f32x4 *)((float *)p.y + at) = v;
-        } else {
-            if (p.residual) {
-                const u32x2 q = *(const u32x2 *)((const uint16_t *)p.residual + at);
-#pragma unroll
-                for (int r = 0; r < 2; ++r) v[2 * r] += bf2f(q[r] & 0xFFFFu), v[2 * r + 1] += bf2f(q[r] >> 16);
-            }
-            *(u32x2 *)((uint16_t *)p.y + at) =
-                (u32x2){f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+    if (p.residual) v = plus_residual<F32>(p, at, n, v);
+    if constexpr (F32) {
+        float *y = (float *)p.y + at;
+        if (n + 4 <= p.N) {
+            *(any_f32x4 *)y = v;
+            return;
         }
-        return;
-    }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        if (n + r >= p.N) return;
-        if constexpr (F32) {
-            if (p.residual) v[r] += ((const float *)p.residual)[at + r];
-            ((float *)p.y)[at + r] = v[r];
-        } else {
-            if (p.residual) v[r] += bf2f(((const uint16_t *)p.residual)[at + r]);
-            ((uint16_t *)p.y)[at + r] = (uint16_t)f2bf(v[r]);
+        for (int e = 0; e < 3; ++e)
+            if (n + e < p.N) y[e] = v[e];
+    } else {
+        uint16_t *y = (uint16_t *)p.y + at;
+        if (n + 4 <= p.N) {
+            *(any_u32x2 *)y = (u32x2){f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+            return;
         }
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (n + e < p.N) y[e] = (uint16_t)f2bf(v[e]);
     }
 }
 

@@ -102,7 +102,7 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
                 *(u32x4 *)(p.hc + (int64_t)(row0 + r) * p.N + n0 + 16 * q) =
                     *(const u32x4 *)(lds + r * kQ + 16 * (q ^ (r & 7)));
         }
-    } else if (splits > 1 || F32 || !p.pieces) {
+    } else if (splits > 1 || F32) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             const int r = wt * TW + 16 * j + c;
@@ -152,12 +152,9 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
                 for (int i = 0; i < NI; ++i) {
                     f32x4 v = acc[i][pass * (TP / 16) + j];
                     const int n = 16 * i + 4 * g;
-                    if (M == Mode::Plain && p.residual && live && n0 + wn * NW + n < p.N) {
-                        const u32x2 q = *(const u32x2 *)((const uint16_t *)p.residual +
-                                                         (row0 + t0 + r) * p.y_stride + n0 + wn * NW + n);
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) v[2 * e] += bf2f(q[e] & 0xFFFFu), v[2 * e + 1] += bf2f(q[e] >> 16);
-                    }
+                    if (M == Mode::Plain && p.residual && live)
+                        v = plus_residual<false>(p, (row0 + t0 + r) * p.y_stride + n0 + wn * NW + n,
+                                                 n0 + wn * NW + n, v);
                     u32x2 two;
                     if constexpr (M == Mode::Down) {
 #pragma unroll
@@ -176,8 +173,12 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
                 const int r = r0 + lane / Q, row = t0 + r;
                 if (row >= rows || n >= p.N) continue;
                 const int64_t t = M == Mode::Down ? p.order[row0 + row] : row0 + row;
-                *(u32x4 *)((uint16_t *)p.y + t * p.y_stride + n) =
-                    *(const u32x4 *)(mine + (r * Q + (q ^ (r & (Q - 1)))) * 16);
+                const u32x4 *from = (const u32x4 *)(mine + (r * Q + (q ^ (r & (Q - 1)))) * 16);
+                uint16_t *y = (uint16_t *)p.y + t * p.y_stride + n;
+                if (M == Mode::Down) *(u32x4 *)y = *from;   // N a multiple of 16
+                else if (n + 8 <= p.N) *(any_u32x4 *)y = *from;
+                else
+                    for (int e = 0; e < p.N - n; ++e) y[e] = ((const uint16_t *)from)[e];
             }
             if (pass + 1 < PASSES) wave_lds();
         }

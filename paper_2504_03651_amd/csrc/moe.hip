@@ -721,7 +721,6 @@ int echo_moe_experts(const echo_experts_t *m, const void *x, const float *x_scal
     dn.KB = IB;
     dn.y = base + w.y;
     dn.y_stride = H;
-    dn.wide = dn.pieces = true;   // H a multiple of 16, y the workspace's
     dn.ye = (int8_t *)(base + w.ye);
     int columns = 0;
     const hipError_t e =

@@ -169,6 +169,31 @@ def test_gemm_adds_the_residual_in_place(T, N, K, f32):
     _check(_gemm(x, xs, w, ws, f32, r, pad=4), want, S + np.abs(r), K, f32)
 
 
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("N", [63, 130, 264])
+@pytest.mark.parametrize("T, K", [(5, 272), (40, 2064), (140, 4096), (300, 400)])
+def test_gemm_into_columns_of_a_wider_matrix(T, N, K, f32, residual):
+    """Rows of y that start at any element, what lies beside them left alone."""
+    import torch
+    from paper_2504_03651_amd import fp8
+    g = np.random.default_rng(T + N)
+    x, xs = activations(g, T, K)
+    w, ws = weights(g, N, K)
+    dt = torch.float32 if f32 else torch.bfloat16
+    full = torch.full((T, N + 7), 3.0, dtype=dt, device="cuda")
+    y = full[:, 1:N + 1]
+    r = bf16_round(g.standard_normal((T, N)).astype(np.float32)) if residual else None
+    if residual:
+        y.copy_(dev(r))
+    n = fp8.gemm_workspace_bytes(T, N, K)
+    fp8.gemm(dev(x), dev(xs), dev(w), dev(ws), y, residual=y if residual else None,
+             workspace=torch.empty(n, dtype=torch.uint8, device="cuda") if n else None)
+    want, S = FO.gemm(x, xs, w, ws, r) if residual else FO.gemm(x, xs, w, ws)
+    _check(y.double().cpu().numpy(), want, S + np.abs(r) if residual else S, K, f32)
+    assert (full[:, 0] == 3.0).all() and (full[:, N + 1:] == 3.0).all()
+
+
 @pytest.mark.parametrize("T", [3, 40, 300])
 def test_gemm_carries_nan_and_infinity_in_their_rows_only(T):
     """A NaN code or an infinite scale of a token reaches that token alone, one of
