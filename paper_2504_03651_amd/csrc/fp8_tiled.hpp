@@ -30,7 +30,8 @@ __device__ __forceinline__ void landed_but() {
 // largest of those columns, at half the bytes of fp32.
 template <Mode M, bool F32, int BN, int BT, int WN, int WT, int ROOM>
 __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
-                                       f32x4 (&acc)[BN / WN / 16][BT / WT / 16], int n_tiles, int nb,
+                                       f32x4 (&acc)[BN / WN / 16][BT / WT / 16],
+                                       const int (&to)[BT / WT / 16], int n_tiles, int nb,
                                        int n0, int row0, int rows, int splits, int split) {
     constexpr int NW = BN / WN, TW = BT / WT, NI = NW / 16, NJ = TW / 16;
     int lane = threadIdx.x & 63;
@@ -107,7 +108,7 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
         for (int j = 0; j < NJ; ++j) {
             const int r = wt * TW + 16 * j + c;
             if (r >= rows) continue;
-            const int64_t t = M == Mode::Down ? p.order[row0 + r] : row0 + r;
+            const int64_t t = row0 + r;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 const int n = n0 + wn * NW + 16 * i + 4 * g;
@@ -146,7 +147,7 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
                     m = fmaxf(m, __shfl_xor(m, 32));
                     up = min(15 - __builtin_amdgcn_frexp_expf(m), 127);   // m 2^up below 2^15
                     if (live && g == 0 && n0 + wn * NW < p.N)
-                        p.ye[p.order[row0 + t0 + r] * (int64_t)p.y_groups + (n0 + wn * NW) / NW] = (int8_t)-up;
+                        p.ye[to[pass * (TP / 16) + j] * (int64_t)p.y_groups + (n0 + wn * NW) / NW] = (int8_t)-up;
                 }
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
@@ -171,8 +172,11 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
 #pragma unroll
             for (int r0 = 0; r0 < TP; r0 += 64 / Q) {
                 const int r = r0 + lane / Q, row = t0 + r;
+                // sixteen rows of one j at most, but for waves of sixteen rows in all
+                static_assert(M != Mode::Down || 64 / Q <= 16 || TW == 16);
+                int64_t t = row0 + row;
+                if constexpr (M == Mode::Down) t = __shfl(to[(pass * TP + r0) / 16], r & 15);
                 if (row >= rows || n >= p.N) continue;
-                const int64_t t = M == Mode::Down ? p.order[row0 + row] : row0 + row;
                 const u32x4 *from = (const u32x4 *)(mine + (r * Q + (q ^ (r & (Q - 1)))) * 16);
                 uint16_t *y = (uint16_t *)p.y + t * p.y_stride + n;
                 if (M == Mode::Down) *(u32x4 *)y = *from;   // N a multiple of 16
@@ -317,6 +321,10 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
     for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    int to[NJ] = {};   // Down: the pairs of this lane's rows
+    if constexpr (M == Mode::Down)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) to[j] = p.order[row0 + min(wt * TW + 16 * j + c, rows - 1)];
     for (int kb = kb0; kb < kb1; ++kb) {
         landed(kb);
         const int free = slot == 0 ? S - 1 : slot - 1;
@@ -361,7 +369,7 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
         take(unit);
         start();
     }
-    finish<M, F32, BN, BT, WN, WT, STAGE>(p, last, acc, n_tiles, nb_, n0_, row0_, rows_, splits, split_);
+    finish<M, F32, BN, BT, WN, WT, STAGE>(p, last, acc, to, n_tiles, nb_, n0_, row0_, rows_, splits, split_);
     if (!again) break;
     }
 }
