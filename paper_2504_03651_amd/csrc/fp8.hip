@@ -206,7 +206,9 @@ __global__ __launch_bounds__(256) void add_parts_kernel(ProductArgs p, int split
 }
 
 // stages of a wave's ring, for NT = 1 and 2
-constexpr int rows_depth(int NT, int XR) { return XR == 8 ? (NT == 1 ? 5 : 3) : XR == 16 ? (NT == 1 ? 4 : 3) : NT == 1 ? 3 : 2; }
+constexpr int rows_depth(int NT, int XR) {
+    return XR == 8 ? (NT == 1 ? 5 : 3) : XR == 16 ? (NT == 1 ? 4 : 3) : NT == 1 ? 3 : 2;
+}
 constexpr int rows_tokens(int T) { return T <= 8 ? 8 : T <= 16 ? 16 : 32; }
 bool rows_fit(int NT, int T, int K) {
     const int XR = rows_tokens(T);
@@ -292,9 +294,11 @@ hipError_t launch_gemm(const ProductArgs &p, Cut c, hipStream_t st) {
         case k64x32: e = launch_tiles<F32, 64, 32, 4, 1, 5>(p, c.splits, st); break;
         case k64x64: e = launch_tiles<F32, 64, 64, 4, 1, 4>(p, c.splits, st); break;
         default:
-            // fp32 results, which take more instructions a product, in tiles of 128
-            // x 64 at most (1,024 x 6144 x 4096: 73 us, in tiles of 128 x 128 90)
-            if (F32 || c.form == k128x64) e = launch_tiles<F32, 128, 64, 4, 1, 3>(p, c.splits, st);
+            // fp32 results, which widen every operand that a wave reads, in waves of
+            // 64 x 64, two workgroups a CU (4,640 x 4096 x 4096: 172 us; in tiles of 128
+            // x 64 with waves of 32 x 64 245, of 128 x 128 with such waves more)
+            if (c.form == k128x64) e = launch_tiles<F32, 128, 64, 4, 1, 3>(p, c.splits, st);
+            else if (F32) e = launch_tiles<true, 128, 128, 2, 2, 2>(p, c.splits, st);
             else if (c.form == k128x128) e = launch_tiles<false, 128, 128, 4, 2, 4>(p, c.splits, st);
             else if (c.form == k256x128) e = launch_tiles<false, 256, 128, 4, 2, 3>(p, c.splits, st);
             else e = launch_tiles<false, 256, 256, 2, 4, 2>(p, c.splits, st);

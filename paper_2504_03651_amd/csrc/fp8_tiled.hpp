@@ -198,13 +198,20 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
 // each of its tokens, and one (GateUp: two) of its weight rows.  Each step's sum
 // comes out of the matrix instruction alone and is scaled on its way into the
 // accumulators, one FMA a value.
+// Bound by LDS: a step of 256 x 256 copies 64 KB in and its waves of 128 x 64 (the
+// largest whose sums fit the registers that FMAs reach) read 192 KB, 1.8 us at the
+// 142 bytes a nanosecond that a CU reads; it takes 1.9, the matrix instructions in it
+// 1.0: 4,640 x 28672 x 4096 in 620 us, 1.76 PFLOP/s.  A step of 256 x 128 takes 1.3.
+// No more workgroups are launched than run at once: each goes on to a next tile,
+// whose first copies it starts before it writes the last one's results (4,640 tokens
+// through 64 experts 510 -> 498 us).
 // ONCE: weights past the caches, where one tile of tokens reads them (8 tokens
 // through 64 experts of 2048 x 1024 66.6 -> 61.5 us, 64 tokens 92 -> 83; 64 x 28672
 // x 4096 35.8 -> 33.4; but two tiles of 64, 100 x 4096 x 4096: 15.5 -> 16.3).
 // part: fp32 sums of one of `splits` equal ranges of K go to part[split][t][n],
 // rows part_pitch apart, instead of y.
 template <Mode M, bool F32, bool ONCE, int BN, int BT, int WN, int WT, int S>
-__global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n_tiles, int t_tiles, int splits) {
+__global__ __launch_bounds__(64 * WN * WT, 512 / (64 * WN * WT)) void tiled_kernel(ProductArgs p, int n_tiles, int t_tiles, int splits) {
     constexpr int W = WN * WT, NW = BN / WN, TW = BT / WT;   // a wave's rows and tokens
     constexpr int NI = NW / 16, NJ = TW / 16;
     constexpr int CODES = (BN + BT) * kQ, STAGE = CODES + 512 * W;
@@ -316,61 +323,61 @@ __global__ __launch_bounds__(64 * WN *WT) void tiled_kernel(ProductArgs p, int n
     take(unit);
     start();
     while (true) {
-    f32x4 acc[NI][NJ];
+        f32x4 acc[NI][NJ];
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    int to[NJ] = {};   // Down: the pairs of this lane's rows
-    if constexpr (M == Mode::Down)
+            for (int j = 0; j < NJ; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        int to[NJ] = {};   // Down: the pairs of this lane's rows
+        if constexpr (M == Mode::Down)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) to[j] = p.order[row0 + min(wt * TW + 16 * j + c, rows - 1)];
-    for (int kb = kb0; kb < kb1; ++kb) {
-        landed(kb);
-        const int free = slot == 0 ? S - 1 : slot - 1;
-        if (kb + S - 1 < kb1) copy(kb + S - 1, free);
-        const uint8_t *stage = lds + slot * STAGE;
-        const uint8_t *wl = stage + (wn * NW + c) * kQ, *xl = stage + (BN + wt * TW + c) * kQ;
-        auto read = [&](const uint8_t *l, int i) {
-            l += 16 * kQ * i;
-            return pair(*(const u32x4 *)(l + at), *(const u32x4 *)(l + (at ^ 64)));
-        };
-        const float *sc = (const float *)(stage + CODES) + 128 * wave;
-        float s[NJ];
+            for (int j = 0; j < NJ; ++j) to[j] = p.order[row0 + min(wt * TW + 16 * j + c, rows - 1)];
+        for (int kb = kb0; kb < kb1; ++kb) {
+            landed(kb);
+            const int free = slot == 0 ? S - 1 : slot - 1;
+            if (kb + S - 1 < kb1) copy(kb + S - 1, free);
+            const uint8_t *stage = lds + slot * STAGE;
+            const uint8_t *wl = stage + (wn * NW + c) * kQ, *xl = stage + (BN + wt * TW + c) * kQ;
+            auto read = [&](const uint8_t *l, int i) {
+                l += 16 * kQ * i;
+                return pair(*(const u32x4 *)(l + at), *(const u32x4 *)(l + (at ^ 64)));
+            };
+            const float *sc = (const float *)(stage + CODES) + 128 * wave;
+            float s[NJ];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[64];
-        // weight rows are read one tile ahead of their products
-        i32x8 b[NJ], a = read(wl, 0);
+            for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[64];
+            // weight rows are read one tile ahead of their products
+            i32x8 b[NJ], a = read(wl, 0);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) b[j] = read(xl, j);
+            for (int j = 0; j < NJ; ++j) b[j] = read(xl, j);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const i32x8 a2 = read(wl, i + 1 < NI ? i + 1 : i);
-            if (M == Mode::GateUp && i == NI / 2)   // on to the up rows
+            for (int i = 0; i < NI; ++i) {
+                const i32x8 a2 = read(wl, i + 1 < NI ? i + 1 : i);
+                if (M == Mode::GateUp && i == NI / 2)   // on to the up rows
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[96];
-            f32x4 v[NJ];
+                    for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[96];
+                f32x4 v[NJ];
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) v[j] = mfma128<F32>(a, b[j]);
+                for (int j = 0; j < NJ; ++j) v[j] = mfma128<F32>(a, b[j]);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[i][j] += v[j] * s[j];
-            a = a2;
+                for (int j = 0; j < NJ; ++j) acc[i][j] += v[j] * s[j];
+                a = a2;
+            }
+            slot = slot + 1 == S ? 0 : slot + 1;
         }
-        slot = slot + 1 == S ? 0 : slot + 1;
-    }
 
-    // the next unit's first steps go to the stages that the last step left free,
-    // and this one's results through the last step's
-    uint8_t *last = lds + (slot == 0 ? S - 1 : slot - 1) * STAGE;
-    const int nb_ = nb, n0_ = n0, row0_ = row0, rows_ = rows, split_ = split;
-    unit += gridDim.x;
-    const bool again = unit < units;
-    if (again) {
-        take(unit);
-        start();
-    }
-    finish<M, F32, BN, BT, WN, WT, STAGE>(p, last, acc, to, n_tiles, nb_, n0_, row0_, rows_, splits, split_);
-    if (!again) break;
+        // the next unit's first steps go to the stages that the last step left free,
+        // and this one's results through the last step's
+        uint8_t *last = lds + (slot == 0 ? S - 1 : slot - 1) * STAGE;
+        const int nb_ = nb, n0_ = n0, row0_ = row0, rows_ = rows, split_ = split;
+        unit += gridDim.x;
+        const bool again = unit < units;
+        if (again) {
+            take(unit);
+            start();
+        }
+        finish<M, F32, BN, BT, WN, WT, STAGE>(p, last, acc, to, n_tiles, nb_, n0_, row0_, rows_, splits, split_);
+        if (!again) break;
     }
 }
 
