@@ -296,7 +296,8 @@ hipError_t launch_gemm(const ProductArgs &p, Cut c, hipStream_t st) {
         default:
             // fp32 results, which widen every operand that a wave reads, in waves of
             // 64 x 64, two workgroups a CU (4,640 x 4096 x 4096: 172 us; in tiles of 128
-            // x 64 with waves of 32 x 64 245, of 128 x 128 with such waves more)
+            // x 64 with waves of 32 x 64 245, and 1,024 x 6144 x 4096 74 and 75, in
+            // tiles of 128 x 128 with such waves 90)
             if (c.form == k128x64) e = launch_tiles<F32, 128, 64, 4, 1, 3>(p, c.splits, st);
             else if (F32) e = launch_tiles<true, 128, 128, 2, 2, 2>(p, c.splits, st);
             else if (c.form == k128x128) e = launch_tiles<false, 128, 128, 4, 2, 4>(p, c.splits, st);
