@@ -67,14 +67,14 @@ typedef struct {
 /* out[t] = (residual[t] +) sum_j weights[t][j] * expert(ids[t][j])(x[t]):
  * x codes [T][H] with scales of 1 x 128 (echo_fp8_quantize), ids and weights
  * [T][top_k], residual (optional; may be out itself) and out bf16 [T][H].
- * Inside an expert the activation SiLU(gate) * up, in fp32, is requantised in
- * blocks of 1 x 128 as echo_fp8_quantize does (quotients within two ulps); an
- * expert's output is rounded to 11 bits (2^-11 of the value, or 2^-39 of the
- * largest of its 16 or more neighbours) before the weighted sum, which is taken in
- * fp32 in the order of j.  A pair whose id lies outside [0, E)
- * adds nothing, whatever its weight: padding, or experts held elsewhere.  An
- * expert may stand twice in a row.  T * top_k at most 2^24; top_k 1..64; T * H
- * and 2 I H below 2^32.
+ * Inside an expert the activation SiLU(gate) * up, in fp32 (of sums as exact as
+ * echo_fp8_gemm's under a bf16 result, or better), is requantised in blocks of
+ * 1 x 128 as echo_fp8_quantize does (quotients within two ulps); an expert's output
+ * is rounded to 11 bits (2^-11 of the value, or 2^-39 of the largest of its 16 or
+ * more neighbours) before the weighted sum, which is taken in fp32 in the order of
+ * j.  A pair whose id lies outside [0, E) adds nothing, whatever its weight:
+ * padding, or experts held elsewhere.  An expert may stand twice in a row.
+ * T * top_k at most 2^24; top_k 1..64; T * H and 2 I H below 2^32.
  * Same inputs give the same bits.  workspace: as for echo_fp8_gemm, of
  * echo_moe_experts_workspace_bytes() bytes. */
 int echo_moe_experts(const echo_experts_t *experts, const void *x, const float *x_scale,

@@ -593,9 +593,15 @@ int launched(const char *what) {
 
 // The forms of both products: the gate and up rows of 128 columns, and rows of
 // the down matrix, by the tile's pairs.  columns: of y under one exponent.
+// The gate and up sums decide codes, and one next to a border falls on either side of
+// it by an e4m3 step.  Tiles of 16 and 32 pairs, which wait for their weights, take
+// these sums from exact products at no cost (8 tokens through 64 experts of 2048 x
+// 1024 59.4 and 59.5 us); larger ones, where a step more or less is one of many and
+// exact products cost time (300 tokens 115 and 134 us, 4,640 505 and 620), take
+// e4m3 products: 1.5e-5 off a sum, and 1.0 to 1.3 times the fp32 form's error behind.
 template <int BT, int GN, int GT, int GS, int BN, int DN, int DT, int DS>
 hipError_t run_experts(const ProductArgs &gu, ProductArgs dn, int max_tiles, int *columns, hipStream_t st) {
-    hipError_t e = launch_tiled<Mode::GateUp, false, (BT <= 64), 256, BT, GN, GT, GS>(gu, max_tiles, 1, st);
+    hipError_t e = launch_tiled<Mode::GateUp, (BT <= 32), (BT <= 64), 256, BT, GN, GT, GS>(gu, max_tiles, 1, st);
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess) return e;
     *columns = BN / DN;
