@@ -337,32 +337,34 @@ __global__ __launch_bounds__(64 * WN * WT, 512 / (64 * WN * WT)) void tiled_kern
             landed(kb);
             const int free = slot == 0 ? S - 1 : slot - 1;
             if (kb + S - 1 < kb1) copy(kb + S - 1, free);
-            const uint8_t *stage = lds + slot * STAGE;
-            const uint8_t *wl = stage + (wn * NW + c) * kQ, *xl = stage + (BN + wt * TW + c) * kQ;
-            auto read = [&](const uint8_t *l, int i) {
-                l += 16 * kQ * i;
-                return pair(*(const u32x4 *)(l + at), *(const u32x4 *)(l + (at ^ 64)));
-            };
-            const float *sc = (const float *)(stage + CODES) + 128 * wave;
-            float s[NJ];
+            if (WT == 1 || wt * TW < rows) {   // this wave has tokens
+                const uint8_t *stage = lds + slot * STAGE;
+                const uint8_t *wl = stage + (wn * NW + c) * kQ, *xl = stage + (BN + wt * TW + c) * kQ;
+                auto read = [&](const uint8_t *l, int i) {
+                    l += 16 * kQ * i;
+                    return pair(*(const u32x4 *)(l + at), *(const u32x4 *)(l + (at ^ 64)));
+                };
+                const float *sc = (const float *)(stage + CODES) + 128 * wave;
+                float s[NJ];
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[64];
-            // weight rows are read one tile ahead of their products
-            i32x8 b[NJ], a = read(wl, 0);
+                for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[64];
+                // weight rows are read one tile ahead of their products
+                i32x8 b[NJ], a = read(wl, 0);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) b[j] = read(xl, j);
+                for (int j = 0; j < NJ; ++j) b[j] = read(xl, j);
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const i32x8 a2 = read(wl, i + 1 < NI ? i + 1 : i);
-                if (M == Mode::GateUp && i == NI / 2)   // on to the up rows
+                for (int i = 0; i < NI; ++i) {
+                    const i32x8 a2 = read(wl, i + 1 < NI ? i + 1 : i);
+                    if (M == Mode::GateUp && i == NI / 2)   // on to the up rows
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[96];
-                f32x4 v[NJ];
+                        for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[96];
+                    f32x4 v[NJ];
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) v[j] = mfma128<F32>(a, b[j]);
+                    for (int j = 0; j < NJ; ++j) v[j] = mfma128<F32>(a, b[j]);
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[i][j] += v[j] * s[j];
-                a = a2;
+                    for (int j = 0; j < NJ; ++j) acc[i][j] += v[j] * s[j];
+                    a = a2;
+                }
             }
             slot = slot + 1 == S ? 0 : slot + 1;
         }
