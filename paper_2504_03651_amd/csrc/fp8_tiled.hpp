@@ -201,7 +201,7 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
 // Bound by LDS: a step of 256 x 256 copies 64 KB in and its waves of 128 x 64 (the
 // largest whose sums fit the registers that FMAs reach) read 192 KB, 1.8 us at the
 // 142 bytes a nanosecond that a CU reads; it takes 1.9, the matrix instructions in it
-// 1.0: 4,640 x 28672 x 4096 in 620 us, 1.76 PFLOP/s.  A step of 256 x 128 takes 1.3.
+// 1.0: 4,640 x 28672 x 4096 in 609 us, 1.79 PFLOP/s.  A step of 256 x 128 takes 1.3.
 // No more workgroups are launched than run at once: each goes on to a next tile,
 // whose first copies it starts before it writes the last one's results (4,640 tokens
 // through 64 experts 510 -> 498 us).
