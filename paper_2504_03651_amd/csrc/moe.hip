@@ -35,14 +35,38 @@ __device__ __forceinline__ bool ahead(V xv, int xi, V yv, int yi) {
     return xv > yv || (xv == yv && xi < yi);
 }
 
+// fp32 as integers of the same order (no NaN; -0 and 0 made equal first)
+__device__ __forceinline__ int ordered(float x) {
+    const int b = __float_as_int(x);
+    return b ^ ((b >> 31) & 0x7FFFFFFF);
+}
+__device__ __forceinline__ float unordered(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
+
+// max over LANES lanes: rotations in rows of 16, then swaps of rows and halves
+template <int LANES>
+__device__ __forceinline__ int lanes_max(int v) {
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, false));   // row_ror:8
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xF, 0xF, false));
+    if constexpr (LANES == 16) return v;
+    const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = max((int)a[0], (int)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    return __builtin_amdgcn_readfirstlane(max((int)b[0], (int)b[1]));
+}
+
 // Of each token, LANES lanes of the wave: groups by the sum of their best one or
 // two of `value` (of all experts, in LDS): the kept ones as bits group * lanes, in
 // `keep`.  LANES / (a power of two of at least that many groups) = `lanes` lanes share
-// a group.  exact: what is in LDS decides; otherwise returns whether the last kept
-// group is more than `apart` times (1 + its magnitude) ahead of the first dropped one.
+// a group.  exact: what is in LDS decides; otherwise values are within off (1 + |value|)
+// of the true ones, and what is returned is whether every kept group is ahead of every
+// dropped one all the same.  A group's sum is then as far off as its values, which
+// may be far larger than the sum: 2 off (1 + the larger magnitude), with the true
+// best two no further from zero than that.
 template <int LANES, typename V>
 __device__ __forceinline__ bool keep_groups(const RouteArgs &a, const V *value, int lanes, int lane,
-                                            bool exact, V apart, uint64_t &keep) {
+                                            bool exact, V off, uint64_t &keep) {
     const int sub = lane & (LANES - 1), from = lane & ~(LANES - 1);
     const int per = a.E / a.groups, g = sub / lanes, in = sub & (lanes - 1);
     V b1 = -INFINITY, b2 = -INFINITY;
@@ -68,9 +92,18 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs &a, const V *value, 
     };
     keep = of(rank < a.top_groups);
     if (exact || a.top_groups == a.groups) return true;
-    const V last = __shfl(v, from + __ffsll((long long)of(rank == a.top_groups - 1)) - 1);
-    const V next = __shfl(v, from + __ffsll((long long)of(rank == a.top_groups)) - 1);
-    return last - next > apart * (1 + (last < 0 ? -last : last));
+    if constexpr (sizeof(V) == 4) {
+        const bool two = a.group_top == 2;
+        // no value, or not two of them: exactly -inf
+        const bool none = b1 == -INFINITY || (two && b2 == -INFINITY && b1 < INFINITY);
+        const V most = two ? fmaxf(fabsf(b1), fabsf(b2)) : fabsf(b1);
+        const V e = none ? 0 : off * (two ? 2 : 1) * (1 + most);
+        const bool clear = of(!none && !(fabsf(v) + e < INFINITY)) == 0;   // no infinity, no NaN
+        const bool mine = in == 0 && g < a.groups, kept = rank < a.top_groups;
+        const int low = ordered(mine && kept ? v - e : INFINITY), high = ordered(mine && !kept ? v + e : -INFINITY);
+        return ~lanes_max<LANES>(~low) > lanes_max<LANES>(high) && clear;
+    }
+    return false;
 }
 
 template <int LANES>
@@ -183,37 +216,19 @@ __device__ __forceinline__ void route_row64(const RouteArgs &a, int64_t t, doubl
     weight = (float)(w * (double)a.scale);
 }
 
-// fp32 as integers of the same order (no NaN; -0 and 0 made equal first)
-__device__ __forceinline__ int ordered(float x) {
-    const int b = __float_as_int(x);
-    return b ^ ((b >> 31) & 0x7FFFFFFF);
-}
-__device__ __forceinline__ float unordered(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
-
-// max over LANES lanes: rotations in rows of 16, then swaps of rows and halves
-template <int LANES>
-__device__ __forceinline__ int lanes_max(int v) {
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, false));   // row_ror:8
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xF, 0xF, false));
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xF, 0xF, false));
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xF, 0xF, false));
-    if constexpr (LANES == 16) return v;
-    const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
-    v = max((int)a[0], (int)a[1]);
-    const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
-    return __builtin_amdgcn_readfirstlane(max((int)b[0], (int)b[1]));
-}
-
 // LANES lanes of a wave per token; lane l of them has experts l, l + LANES, ...
 // Without a bias the keys are the logits, exact in fp32.  With one (or where groups
 // go by sums of scores) the keys come in fp32, off by less than off (1 + |key|): for
 // a sigmoid s = 1 / (1 + e), e = e^-z comes (|z| + 2) 2^-24 off, which makes s (1 - s)
 // (|z| + 2) 2^-24 < 0.75 x 2^-24 of it, the sum and the hardware's reciprocal 3 x
-// 2^-24 s, with the rounding of the key below 5 x 2^-24; for a softmax at most 20
-// roundings of a score (its exponential's, the sum's over the lanes, the
-// reciprocal's), below 2^-19.  Where two neighbours among the chosen and the next,
-// or the groups at the border, are not further apart than that the row goes to
-// route_row64.  The chosen experts' scores are taken in 64 bits.
+// 2^-24 s, with the rounding of the key below 5 x 2^-24, taken as 8; for a softmax,
+// with d = top - z, e^-d comes (d + 6) 2^-24 off (expf within three ulps), the sum the
+// mean of that over its terms (d: 3.9 at most, of 512) and a rounding for each
+// of a lane's PER additions and each step over the lanes, then two roundings, and e^-d
+// d is at most 0.37: below PER + log2(LANES) + 18 times 2^-24, the 18 taken as 24.  Where
+// two neighbours among the chosen and the next, or a kept group and a dropped one,
+// are not further apart than that the row goes to route_row64.  The chosen experts'
+// scores are taken in 64 bits.
 // Bound by instructions, and where rows go to route_row64 by its 5.5 us: 16,412
 // tokens of 256 experts, 8 chosen of 4 groups of 8 with a bias, take 25 us (34 with a
 // wave a token, 60 all in 64 bits).
@@ -227,7 +242,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
     const int64_t t0 = ((int64_t)blockIdx.x * 4 + wave) * TOKENS;
     if (t0 >= a.T) return;
     const int64_t t = min(t0 + lane / LANES, (int64_t)a.T - 1);
-    constexpr float off = SIGMOID ? 0x1p-21f : 0x1p-19f;
+    constexpr float off = 0x1p-24f * (SIGMOID ? 8 : PER + (LANES == 16 ? 4 : 6) + 24);
     // of a wave: E doubles, or E floats of each token
     double *row = route_lds + wave * a.E * (TOKENS > 1 ? TOKENS / 2 : 1);
     float z[PER];
@@ -293,7 +308,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a) {
         wave_lds();
         uint64_t keep;
         sure = keep_groups<LANES, float>(a, (const float *)row + lane / LANES * a.E, lanes, lane,
-                                         !a.bias && !sums, 4 * off, keep);
+                                         !a.bias && !sums, off, keep);
         const uint32_t per = a.E / a.groups, inv = ((1u << 20) + per - 1) / per;   // e / per, e < 512
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
