@@ -50,7 +50,9 @@ int echo_fp8_quantize(const void *x, int32_t x_dtype, int64_t x_stride, int32_t 
  * in_features) with scales of 128 x 128, sums in fp32, y [T][N] bf16 or fp32
  * with rows y_stride >= N elements apart, rounded once (under a bf16 result the
  * e4m3 matrix instructions add 128 products to about 1.5e-5 of the sum; an fp32
- * result takes exact products and fp32 sums).  residual (optional):
+ * result takes exact products and fp32 sums).  Scales may be any fp32 numbers: it is
+ * the scaled sum of a block that has to be one, not the product of its scales.
+ * residual (optional):
  * of y's type and strides, added before that rounding; it may be y itself, and
  * overlaps it in no other way; y overlaps no other buffer.  K a multiple of 16,
  * at most 2^23; x and w 16-byte aligned.

@@ -83,18 +83,30 @@ __global__ __launch_bounds__(64 * kStreamWaves) void stream_kernel(ProductArgs p
         const int b = kb - kb0;
         const float sw = wsl[b];
         i32x8 a[NT], x[TT];
-        float s[TT];
+        float s[TT], sx[TT];
+        bool odd = false;
 #pragma unroll
         for (int i = 0; i < NT; ++i) a[i] = read(16 * i + c);
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
             x[t] = read(16 * NT + (XR == 8 ? c & 7 : 16 * t + c));
-            s[t] = xsl[(b / 4 * TT + t) * 64 + b % 4 * 16 + c] * sw;
+            sx[t] = xsl[(b / 4 * TT + t) * 64 + b % 4 * 16 + c];
+            s[t] = sx[t] * sw;
+            odd |= odd_scale(s[t]);
         }
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int t = 0; t < TT; ++t) acc[i][t] += mfma128<F32>(a[i], x[t]) * s[t];
+            for (int t = 0; t < TT; ++t) acc[i][t] += mfma128<F32>(a[i], x[t]) * (odd_scale(s[t]) ? 0.f : s[t]);
+        if (__any(odd)) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int t = 0; t < TT; ++t) {
+                    const f32x4 v = scaled(mfma128<F32>(a[i], x[t]), sx[t], sw);
+                    if (odd_scale(s[t])) acc[i][t] += v;
+                }
+        }
         // the stage has been read: its operands are in registers
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (kb + D < kb1) copy(kb + D, slot);

@@ -333,6 +333,7 @@ __global__ __launch_bounds__(64 * WN * WT, 512 / (64 * WN * WT)) void tiled_kern
         if constexpr (M == Mode::Down)
 #pragma unroll
             for (int j = 0; j < NJ; ++j) to[j] = p.order[row0 + min(wt * TW + 16 * j + c, rows - 1)];
+        uint32_t least = kOddClass;   // of the scales that this lane's sums took
         for (int kb = kb0; kb < kb1; ++kb) {
             landed(kb);
             const int free = slot == 0 ? S - 1 : slot - 1;
@@ -346,8 +347,14 @@ __global__ __launch_bounds__(64 * WN * WT, 512 / (64 * WN * WT)) void tiled_kern
                 };
                 const float *sc = (const float *)(stage + CODES) + 128 * wave;
                 float s[NJ];
+                auto scales = [&](int at) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[64];
+                    for (int j = 0; j < NJ; ++j) {
+                        s[j] = sc[16 * j + c] * sc[at];
+                        least = min(least, scale_class(s[j]));
+                    }
+                };
+                scales(64);
                 // weight rows are read one tile ahead of their products
                 i32x8 b[NJ], a = read(wl, 0);
 #pragma unroll
@@ -355,9 +362,7 @@ __global__ __launch_bounds__(64 * WN * WT, 512 / (64 * WN * WT)) void tiled_kern
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
                     const i32x8 a2 = read(wl, i + 1 < NI ? i + 1 : i);
-                    if (M == Mode::GateUp && i == NI / 2)   // on to the up rows
-#pragma unroll
-                        for (int j = 0; j < NJ; ++j) s[j] = sc[16 * j + c] * sc[96];
+                    if (M == Mode::GateUp && i == NI / 2) scales(96);   // on to the up rows
                     f32x4 v[NJ];
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) v[j] = mfma128<F32>(a, b[j]);
@@ -367,6 +372,46 @@ __global__ __launch_bounds__(64 * WN * WT, 512 / (64 * WN * WT)) void tiled_kern
                 }
             }
             slot = slot + 1 == S ? 0 : slot + 1;
+        }
+        if (__any(least < kOddClass)) {
+            // Some were no normal numbers: the wave takes its sums again, straight from
+            // memory, a matrix instruction at a time.
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    int lane = threadIdx.x & 63;
+                    asm volatile("" : "+v"(lane));   // addresses live for their products only
+                    const int g = lane >> 4, c = lane & 15;
+                    int n = wn * NW + 16 * i + c, r = min(wt * TW + 16 * j + c, rows - 1);
+                    const float *sw = ws;
+                    if constexpr (M == Mode::GateUp) {
+                        const bool up = i >= NI / 2;
+                        n = min(n0 + wn * (NW / 2) + 16 * (i % (NI / 2)) + c, p.N - 1) + (up ? p.N : 0);
+                        r = p.order[row0 + r] / p.top_k;
+                        if (up && lane < 32) sw += (int64_t)n_tiles * p.KB;
+                        if (!up && lane >= 32) sw -= (int64_t)n_tiles * p.KB;
+                    } else {
+                        n = min(n, p.N - 1 - n0);
+                    }
+                    const uint8_t *w = wsrc + (int64_t)n * p.K, *x = xsrc + (int64_t)r * p.K;
+                    const float *sx = xscale + (int64_t)r * p.KB;
+                    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        const int64_t at = (int64_t)kQ * kb + 16 * g;
+                        u32x4 a[2], b[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const bool in = at + 64 * h < p.K;
+                            a[h] = in ? *(const u32x4 *)(w + at + 64 * h) : (u32x4){0u, 0u, 0u, 0u};
+                            b[h] = in ? *(const u32x4 *)(x + at + 64 * h) : (u32x4){0u, 0u, 0u, 0u};
+                        }
+                        v += scaled(mfma128<F32>(pair(a[0], a[1]), pair(b[0], b[1])), sx[kb], sw[kb]);
+                    }
+                    acc[i][j] = v;
+                }
+            }
         }
 
         // the next unit's first steps go to the stages that the last step left free,
