@@ -64,7 +64,9 @@ int echo_fp8_gemm(const void *x, const float *x_scale, const void *w, const floa
                   void *workspace, size_t workspace_bytes, void *stream);
 
 /* Workspace bytes echo_fp8_gemm needs for these sizes: 0 where it needs none
- * or the sizes are invalid (with a detail in echo_last_error() then). */
+ * or the sizes are invalid (with a detail in echo_last_error() then).  They do not
+ * fall with num_tokens: what the largest batch needs serves every smaller one.  At
+ * most 256 MiB. */
 size_t echo_fp8_gemm_workspace_bytes(int32_t num_tokens, int32_t out_features,
                                      int32_t in_features);
 

@@ -222,14 +222,47 @@ struct Cut {
     int splits;
 };
 
+// Tiles n x t: what a step of 128 of K takes with one workgroup on a CU, and with two
+// where LDS holds two
+constexpr struct {
+    Form form;
+    int n, t;
+    double one, two;
+} kTileForms[] = {{k64x32, 64, 32, .37, .52},   {k64x64, 64, 64, .45, .75}, {k128x64, 128, 64, .68, 1.0},
+                  {k128x128, 128, 128, .88, 0}, {k256x128, 256, 128, 1.32, 0}, {k256x256, 256, 256, 2.4, 0}};
+constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16};
+
+// Products of more tiles, or whose parts would take more, are not cut into ranges of K
+// (of 2 million sizes of K up to 19,200 none would be), so that there is a bound on
+// the parts of every product of up to T tokens.
+constexpr int kRangeTiles = 2048;
+constexpr size_t kPartBytes = 256u << 20;
+
+// columns of a row of parts
+int pitch_of(int N) { return (int)(((int64_t)N + 3) / 4 * 4); }
+size_t parts_bytes(int splits, int T, int N) { return splits == 1 ? 0 : (size_t)splits * T * pitch_of(N) * 4; }
+
+// The most bytes of parts of up to T tokens.  A form's tiles in s ranges are at most
+// kRangeTiles: with m = kRangeTiles / its tiles of N, s times its tiles of tokens is at
+// most m, and s times the tokens at most m t.
+size_t most_parts_bytes(int T, int N, int K) {
+    int s_most = 1;
+    for (int s : kRanges)
+        if (2 * s <= cdiv(K, kQ)) s_most = s;
+    int64_t rows = 0;   // s times the tokens
+    for (const auto &f : kTileForms) {
+        const int m = kRangeTiles / cdiv(N, f.n);
+        if (m > 1 && s_most > 1) rows = std::max(rows, std::min((int64_t)std::min(s_most, m) * T, (int64_t)m * f.t));
+    }
+    return std::min<size_t>((size_t)rows * pitch_of(N) * 4, kPartBytes);
+}
+
 // The cut of least estimated time, in microseconds fitted to 130 sizes (T 1 to
 // 4,640, N x K from 512 x 512 to 28672 x 4096, weights from memory).
 //   Weights and tokens come at 5.2 TB/s at most.
 //   kRows: 16 or 32 weight rows a workgroup, every wave on its own; one workgroup a
 //   CU, which takes in 50 KB a microsecond, tokens among them (8 x 6144 x 4096: 9.0
 //   by 32 rows, 11.0 by 16; 8 x 4096 x 4096: 8.0 and 7.2).
-//   Tiles n x t: what a step of 128 of K takes with one workgroup on a CU, and
-//   with two where LDS holds two.
 //   Ranges of K cost a second launch and their fp32 parts' way to memory and back
 //   (137 x 4096 x 14336: 95 in one range, 30.7 to 32 in eight).
 Cut cut_of(int T, int N, int K) {
@@ -245,17 +278,12 @@ Cut cut_of(int T, int N, int K) {
                           1.5 * (double)(turns - 1);
         if (us < least) least = us, best = Cut{nt == 1 ? kRows16 : kRows32, 1};
     }
-    static const struct {
-        Form form;
-        int n, t;
-        double one, two;
-    } tiles[] = {{k64x32, 64, 32, .37, .52},   {k64x64, 64, 64, .45, .75}, {k128x64, 128, 64, .68, 1.0},
-                 {k128x128, 128, 128, .88, 0}, {k256x128, 256, 128, 1.32, 0}, {k256x256, 256, 256, 2.4, 0}};
-    for (const auto &f : tiles) {
+    for (const auto &f : kTileForms) {
         if (f.t > 32 && T <= f.t / 2) continue;
-        for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
-            if (s > 1 && 2 * s > KB) break;
-            const int64_t each = ((int64_t)cdiv(N, f.n) * cdiv(T, f.t) * s + 255) / 256;   // of a CU
+        for (int s : kRanges) {
+            const int64_t all = (int64_t)cdiv(N, f.n) * cdiv(T, f.t) * s;
+            if (s > 1 && (2 * s > KB || all > kRangeTiles || parts_bytes(s, T, N) > kPartBytes)) break;
+            const int64_t each = (all + 255) / 256;   // of a CU
             const double turns = f.two > 0 ? (double)(each / 2) * f.two + (double)(each % 2) * f.one
                                            : (double)each * f.one;
             const double starts = (double)(f.two > 0 ? (each + 1) / 2 : each) - 1;
@@ -323,13 +351,6 @@ int launched(const char *what) {
     return e == hipSuccess ? ECHO_OK : fail(ECHO_E_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-// columns of a row of parts
-int pitch_of(int32_t N) { return (int)(((int64_t)N + 3) / 4 * 4); }
-
-size_t parts_bytes(Cut c, int32_t T, int32_t N) {
-    return c.splits == 1 ? 0 : (size_t)c.splits * T * pitch_of(N) * 4;
-}
-
 int check_sizes(int32_t T, int32_t N, int32_t K) {
     if (T < 0) return fail(ECHO_E_INVALID, "num_tokens %d", T);
     if (N <= 0 || K <= 0) return fail(ECHO_E_INVALID, "out_features %d, in_features %d", N, K);
@@ -393,7 +414,7 @@ size_t echo_fp8_gemm_workspace_bytes(int32_t num_tokens, int32_t out_features,
                                      int32_t in_features) {
     clear_error();
     if (check_sizes(num_tokens, out_features, in_features) || num_tokens == 0) return 0;
-    return parts_bytes(cut_of(num_tokens, out_features, in_features), num_tokens, out_features);
+    return most_parts_bytes(num_tokens, out_features, in_features);
 }
 
 int echo_fp8_gemm(const void *x, const float *x_scale, const void *w, const float *w_scale,
@@ -417,7 +438,7 @@ int echo_fp8_gemm(const void *x, const float *x_scale, const void *w, const floa
     if (((uintptr_t)x_scale | (uintptr_t)w_scale) & 3u || ya & (y_dtype == ECHO_F32 ? 3u : 1u))
         return fail(ECHO_E_INVALID, "scales, y and residual must have their types' alignment");
     const Cut cut = cut_of(num_tokens, out_features, in_features);
-    const size_t need = parts_bytes(cut, num_tokens, out_features);
+    const size_t need = most_parts_bytes(num_tokens, out_features, in_features);
     if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u)))
         return fail(ECHO_E_WORKSPACE, "workspace of %zu bytes (need %zu, 256-byte aligned)",
                     workspace_bytes, need);

@@ -137,6 +137,7 @@ def quantize(x, codes, scales, block_rows: int = 1, stream=None) -> None:
 
 
 def gemm_workspace_bytes(num_tokens: int, out_features: int, in_features: int) -> int:
+    """Enough for every product of up to ``num_tokens`` tokens with such weights."""
     n = int(_lib().echo_fp8_gemm_workspace_bytes(int(num_tokens), int(out_features),
                                                  int(in_features)))
     if n == 0 and echo.last_error():
