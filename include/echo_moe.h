@@ -83,7 +83,8 @@ int echo_moe_experts(const echo_experts_t *experts, const void *x, const float *
                      void *stream);
 
 /* Workspace bytes echo_moe_experts needs (0 and a detail in echo_last_error()
- * when the arguments are invalid; 0 for no tokens). */
+ * when the arguments are invalid; 0 for no tokens).  They do not fall with
+ * num_tokens. */
 size_t echo_moe_experts_workspace_bytes(const echo_experts_t *experts, int32_t num_tokens,
                                         int32_t top_k);
 

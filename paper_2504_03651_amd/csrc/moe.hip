@@ -591,7 +591,7 @@ int plan_ws(const echo_experts_t *x, int32_t T, int32_t top_k, Ws *w) {
     w->chunks = cdiv(R, w->chunk);
     w->num_tiles = take(4);
     w->counts = take(4 * (size_t)E * w->chunks);
-    w->tiles = take(sizeof(Tile) * w->max_tiles);
+    w->tiles = take(sizeof(Tile) * (R / 16 + std::min<int64_t>(E, R)));   // as for the smallest: no fall with T
     w->order = take(4 * R);
     w->hs = take(4 * R * cdiv(x->intermediate, kQ));
     w->hc = take(R * x->intermediate);
