@@ -57,7 +57,7 @@ int echo_moe_route(const echo_router_t *router, const void *logits, int32_t logi
 typedef struct {
     int32_t num_experts;           /* E, 1..512 */
     int32_t hidden;                /* H, a multiple of 16 */
-    int32_t intermediate;          /* I, a multiple of 16 */
+    int32_t intermediate;          /* I, a multiple of 16, at most 2^23 */
     const void *w_gate_up;         /* [E][2 I][H]: gate rows, then up rows */
     const float *gate_up_scale;    /* [E][2][IB][HB] */
     const void *w_down;            /* [E][H][I] */

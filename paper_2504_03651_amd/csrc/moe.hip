@@ -564,9 +564,12 @@ int plan_ws(const echo_experts_t *x, int32_t T, int32_t top_k, Ws *w) {
         return fail(ECHO_E_UNSUPPORTED, "num_experts %d (1..%d)", x->num_experts, kMaxExperts);
     if (x->hidden <= 0 || x->intermediate <= 0)
         return fail(ECHO_E_INVALID, "hidden %d, intermediate %d", x->hidden, x->intermediate);
-    if (x->hidden % 16 || x->intermediate % 16 || x->intermediate > INT32_MAX / 2)
+    if (x->hidden % 16 || x->intermediate % 16)
         return fail(ECHO_E_UNSUPPORTED, "hidden %d and intermediate %d must be multiples of 16",
                     x->hidden, x->intermediate);
+    // offsets inside a tile of rows of `intermediate` codes are 32 bits
+    if (x->intermediate > 1 << 23)
+        return fail(ECHO_E_UNSUPPORTED, "intermediate %d above %d", x->intermediate, 1 << 23);
     if (T < 0) return fail(ECHO_E_INVALID, "num_tokens %d", T);
     if (top_k < 1 || top_k > kMaxTopK) return fail(ECHO_E_INVALID, "top_k %d (1..%d)", top_k, kMaxTopK);
     const int64_t R = (int64_t)T * top_k;
