@@ -693,13 +693,14 @@ int echo_moe_experts(const echo_experts_t *m, const void *x, const float *x_scal
         return fail(ECHO_E_INVALID, "an expert weight or scale is NULL");
     if (((uintptr_t)m->w_gate_up | (uintptr_t)m->w_down) & 15u)
         return fail(ECHO_E_INVALID, "expert weights must be 16-byte aligned");
+    if (((uintptr_t)m->gate_up_scale | (uintptr_t)m->down_scale) & 3u)
+        return fail(ECHO_E_INVALID, "expert scales are not aligned to their type");
     if (num_tokens == 0) return ECHO_OK;
     if (!x || !x_scale || !ids || !weights || !out)
         return fail(ECHO_E_INVALID, "x, x_scale, ids, weights or out is NULL");
     if (((uintptr_t)x | (uintptr_t)out | (uintptr_t)residual) & 15u)
         return fail(ECHO_E_INVALID, "x, residual and out must be 16-byte aligned");
-    if (((uintptr_t)x_scale | (uintptr_t)ids | (uintptr_t)weights | (uintptr_t)m->gate_up_scale |
-         (uintptr_t)m->down_scale) & 3u)
+    if (((uintptr_t)x_scale | (uintptr_t)ids | (uintptr_t)weights) & 3u)
         return fail(ECHO_E_INVALID, "a buffer is not aligned to its type");
     if (!workspace || workspace_bytes < w.total || ((uintptr_t)workspace & 255u))
         return fail(ECHO_E_WORKSPACE, "workspace of %zu bytes (need %zu, 256-byte aligned)",
@@ -755,8 +756,7 @@ int echo_moe_experts(const echo_experts_t *m, const void *x, const float *x_scal
                        : run_experts<16, 8, 1, 2, 64, 4, 1, 4>(gu, dn, w.max_tiles, &columns, st);
     if (e != hipSuccess) return fail(ECHO_E_HIP, "experts' products: %s", hipGetErrorString(e));
     if ((rc = launched("experts' products"))) return rc;
-    const int64_t n8 = (int64_t)num_tokens * H / 8;
-    if (n8 > 256 * (int64_t)INT32_MAX) return fail(ECHO_E_UNSUPPORTED, "output too large");
+    const int64_t n8 = (int64_t)num_tokens * H / 8;   // below 2^29
     hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((n8 + 255) / 256)), dim3(256), 0, st,
                        (const uint16_t *)(base + w.y), dn.ye, __builtin_ctz(columns), ids, weights, (const uint16_t *)residual,
                        (uint16_t *)out, n8, H, E, top_k);
