@@ -562,6 +562,17 @@ int attn_device_planned(const echo_kv_pool_t *pool, const echo_batch_t *batch, c
     return launch_attention(pool, batch, q, num_q_heads, sm_scale, out, a, s, ev);
 }
 
+// *most: blocks of the longest prefill row
+int check_prefill_blocks(const echo_kv_pool_t *pool, const Plan &plan, int32_t *most) {
+    *most = 0;
+    for (const PrefillDesc &d : plan.pdesc)
+        *most = std::max(*most, (d.key_end + kBlock - 1) / kBlock - d.key_begin / kBlock);
+    if (*most > prefill_max_blocks(pool->head_dim))
+        return fail(ECHO_E_UNSUPPORTED, "prefill row of %d blocks exceeds the %d-block limit", *most,
+                    prefill_max_blocks(pool->head_dim));
+    return ECHO_OK;
+}
+
 // Enqueues a host-planned call of checked arguments.
 int attn_planned(const echo_kv_pool_t *pool, const echo_batch_t *batch, const void *q,
                  int32_t num_q_heads, float sm_scale, float *out, void *workspace,
@@ -569,11 +580,7 @@ int attn_planned(const echo_kv_pool_t *pool, const echo_batch_t *batch, const vo
                  hipStream_t s, const Plan &plan) {
     const PlanLayout &L = plan.layout;
     int32_t pf_blocks = 0;
-    for (const PrefillDesc &d : plan.pdesc)
-        pf_blocks = std::max(pf_blocks, (d.key_end + kBlock - 1) / kBlock - d.key_begin / kBlock);
-    if (pf_blocks > prefill_max_blocks(pool->head_dim))
-        return fail(ECHO_E_UNSUPPORTED, "prefill row of %d blocks exceeds the %d-block limit",
-                    pf_blocks, prefill_max_blocks(pool->head_dim));
+    if (const int long_row = check_prefill_blocks(pool, plan, &pf_blocks)) return long_row;
     const size_t need = (size_t)L.total_words * 4;
     if (!workspace || workspace_bytes < need)
         return fail(ECHO_E_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, need);
@@ -642,6 +649,34 @@ int attn_planned(const echo_kv_pool_t *pool, const echo_batch_t *batch, const vo
 }
 
 }  // namespace
+
+// Both workspaces of echo_attn_mixed from one plan, and what it would refuse the
+// batch for (host: 0 without mirrors).
+int echo::attn_bytes(const echo_kv_pool_t *pool, const echo_batch_t *batch, int32_t num_q_heads,
+                     size_t *device, size_t *host) {
+    *device = 256;
+    *host = 0;
+    int rc = check_attn_args(pool, batch, num_q_heads);
+    if (rc || batch->num_rows == 0) return rc;
+    if (!has_mirrors(batch)) {
+        DevLayout L;
+        if ((rc = dev_layout(pool, batch, num_q_heads, L))) return rc;
+        *device = (size_t)L.total_words * 4;
+        return ECHO_OK;
+    }
+    thread_local Plan plan;
+    int32_t most = 0;
+    if ((rc = plan_checked(pool, batch, num_q_heads, plan))) return rc;
+    if ((rc = check_prefill_blocks(pool, plan, &most))) return rc;
+    *device = (size_t)plan.layout.total_words * 4;
+    *host = (size_t)plan.layout.upload_words * 4;
+    return ECHO_OK;
+}
+
+int echo::check_attn_host(void *host_workspace, size_t bytes, size_t need) {
+    void *on_device = nullptr;
+    return need ? check_host_workspace(host_workspace, bytes, need, &on_device) : ECHO_OK;
+}
 
 extern "C" {
 

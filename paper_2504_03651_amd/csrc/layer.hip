@@ -228,6 +228,7 @@ int gemm(Blas *bl, int64_t N, int64_t T, int64_t K, const void *W, const void *X
 
 struct Ws {
     size_t y, qkv, q, kn, vn, attn, attn_ws, attn16, h, gu, act, blas, total;
+    size_t attn_host;   // bytes of host workspace
 };
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -250,8 +251,8 @@ int plan_ws(const echo_layer_t *L, const echo_kv_pool_t *pool, const echo_batch_
     const int64_t T = b->num_tokens, H = L->hidden, I = L->intermediate;
     const int64_t qd = (int64_t)L->num_q_heads * L->head_dim;
     const int64_t kd = (int64_t)L->num_kv_heads * L->head_dim;
-    const size_t attn_ws = echo_attn_workspace_bytes(pool, b, L->num_q_heads);
-    if (attn_ws == 0 && b->num_rows > 0) return ECHO_E_INVALID;   // detail already set
+    size_t attn_ws = 0;
+    if ((rc = echo::attn_bytes(pool, b, L->num_q_heads, &attn_ws, &w->attn_host))) return rc;
     size_t o = 0;
     auto take = [&](size_t n) { const size_t at = o; o += up256(n); return at; };
     w->y = take(T * H * 2);
@@ -272,6 +273,7 @@ int plan_ws(const echo_layer_t *L, const echo_kv_pool_t *pool, const echo_batch_
 
 struct MoeWs {
     size_t y, codes, scales, qkv, q, kn, vn, attn, attn_ws, h, logits, ids, weights, scratch, total;
+    size_t attn_host;   // bytes of host workspace
 };
 
 // (the caller clears the error detail first)
@@ -304,8 +306,8 @@ int plan_moe_ws(const echo_moe_layer_t *L, const echo_kv_pool_t *pool, const ech
     const int64_t qd = (int64_t)L->num_q_heads * L->head_dim;
     const int64_t kd = (int64_t)L->num_kv_heads * L->head_dim;
     if (qd + 2 * kd > INT32_MAX) return fail(ECHO_E_UNSUPPORTED, "%lld columns of qkv", (long long)(qd + 2 * kd));
-    const size_t attn_ws = echo_attn_workspace_bytes(pool, b, L->num_q_heads);
-    if (attn_ws == 0 && b->num_rows > 0) return ECHO_E_INVALID;   // detail already set
+    size_t attn_ws = 0;
+    if ((rc = echo::attn_bytes(pool, b, L->num_q_heads, &attn_ws, &w->attn_host))) return rc;
     // one scratch for the products, the router's library product and the experts
     size_t scratch = kBlasWs;
     const int64_t shapes[2][2] = {{qd + 2 * kd, H}, {H, qd}};
@@ -388,6 +390,7 @@ int echo_layer_forward(const echo_layer_t *L, const echo_kv_pool_t *pool,
     if (!workspace || workspace_bytes < w.total || ((uintptr_t)workspace & 255u))
         return fail(ECHO_E_WORKSPACE, "workspace of %zu bytes (need %zu, 256-byte aligned)",
                     workspace_bytes, w.total);
+    if ((rc = echo::check_attn_host(host_workspace, host_workspace_bytes, w.attn_host))) return rc;
     Blas *bl = nullptr;
     if ((rc = get_blas(&bl))) return rc;
     hipStream_t st = (hipStream_t)stream;
@@ -482,6 +485,7 @@ int echo_moe_layer_forward(const echo_moe_layer_t *L, const echo_kv_pool_t *pool
     if (!workspace || workspace_bytes < w.total || ((uintptr_t)workspace & 255u))
         return fail(ECHO_E_WORKSPACE, "workspace of %zu bytes (need %zu, 256-byte aligned)",
                     workspace_bytes, w.total);
+    if ((rc = echo::check_attn_host(host_workspace, host_workspace_bytes, w.attn_host))) return rc;
     Blas *bl = nullptr;
     if ((rc = get_blas(&bl))) return rc;
     hipStream_t st = (hipStream_t)stream;

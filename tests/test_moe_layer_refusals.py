@@ -20,3 +20,24 @@ def test_expert_scales_off_their_alignment(scale):
     assert layer._lib().echo_moe_layer_workspace_bytes(*args) == 0 and "aligned" in echo.last_error()
     assert layer._lib().echo_moe_layer_forward(*args, P, P, 1 << 40, None, 0, None) == INV
     assert "aligned" in echo.last_error()
+
+
+def _dense():
+    from paper_2504_03651_amd import layer
+    return layer, layer.CLayer(256, 4, 4, 64, 128, 1e4, 1e-5, P, P, P, P, P, P)
+
+
+@pytest.mark.parametrize("name", ["echo_moe_layer_forward", "echo_layer_forward"])
+@pytest.mark.parametrize("short", [None, 16])
+def test_host_workspace_is_checked_before_anything_is_enqueued(name, short):
+    """The attention's plan needs host memory: a layer without it, or with too little,
+    is refused before the cache is touched (before any library handle or launch, too:
+    there is no GPU here)."""
+    layer, c = _moe_layer() if "moe" in name else _dense()
+    cp, cb, keep = echo.host_structs(W.config1())
+    need = echo.lib().echo_attn_host_workspace_bytes(ctypes.byref(cp), ctypes.byref(cb), 4)
+    assert need > 16
+    host = ctypes.create_string_buffer(64)
+    rc = getattr(layer._lib(), name)(ctypes.byref(c), ctypes.byref(cp), ctypes.byref(cb), P, P, 1 << 40,
+                                     None if short is None else ctypes.addressof(host), short or 0, None)
+    assert rc == echo.ECHO_E_WORKSPACE and "host workspace" in echo.last_error(), echo.last_error()
