@@ -42,6 +42,13 @@ def refuse(where: str, what: str):
     raise echo.EchoError(echo.ECHO_E_INVALID, where, what)
 
 
+def sizes(where: str, *n: int):
+    """Refuses counts that the library's 32-bit arguments would cut off."""
+    for v in n:
+        if not -2 ** 31 <= v < 2 ** 31:
+            refuse(where, f"{v} is not below 2^31")
+
+
 class _Types:
     """Types that tensors may have (filled in at the first call: importing this
     module does not import torch)."""
@@ -122,9 +129,13 @@ def quantize(x, codes, scales, block_rows: int = 1, stream=None) -> None:
         raise echo.EchoError(echo.ECHO_E_UNSUPPORTED, where, f"block_rows {block_rows}")
     if len(shape) == 2:
         batch, (n, cols), lead = 1, shape, ()
+        if (n | cols) >> 31:
+            sizes(where, n, cols)
         xp, stride = rows(where, "x", x, shape, k.real, dev)
     elif len(shape) == 3:
         batch, n, cols = shape
+        if (batch | n | cols) >> 31:
+            sizes(where, batch, n, cols)
         xp, stride, lead = address(where, "x", x, shape, k.real, dev), cols, (batch,)
     else:
         refuse(where, f"x has {x.dim()} axes")
@@ -138,6 +149,7 @@ def quantize(x, codes, scales, block_rows: int = 1, stream=None) -> None:
 
 def gemm_workspace_bytes(num_tokens: int, out_features: int, in_features: int) -> int:
     """Enough for every product of up to ``num_tokens`` tokens with such weights."""
+    sizes("echo_fp8_gemm_workspace_bytes", num_tokens, out_features, in_features)
     n = int(_lib().echo_fp8_gemm_workspace_bytes(int(num_tokens), int(out_features),
                                                  int(in_features)))
     if n == 0 and echo.last_error():
@@ -155,6 +167,8 @@ def gemm(x, x_scale, w, w_scale, out, residual=None, workspace=None, stream=None
     if x.dim() != 2 or w.dim() != 2:
         refuse(where, f"x has {x.dim()} axes, w {w.dim()}")
     (T, K), N = x.shape, w.shape[0]
+    if (T | K | N) >> 31:
+        sizes(where, T, K, N)
     kb = -(-K // BLOCK)
     xp = address(where, "x", x, (T, K), k.codes, dev)
     xsp = address(where, "x_scale", x_scale, (T, kb), k.f32, dev)

@@ -51,6 +51,7 @@ class Router:
                  scale: float = 1.0):
         if score not in SCORES:
             raise echo.EchoError(echo.ECHO_E_UNSUPPORTED, "Router", f"score {score!r}")
+        fp8.sizes("Router", num_experts, top_k, num_groups, top_groups, group_top)
         self.num_experts, self.top_k = num_experts, top_k
         self.c = CRouter(num_experts, top_k, SCORES[score], num_groups, top_groups, group_top,
                          int(renormalize), scale)
@@ -62,7 +63,11 @@ def route(router: Router, logits, ids, weights, bias=None, stream=None) -> None:
     ``logits`` [T][E] (bf16 or fp32, rows any distance apart); ``bias``: fp32 [E]."""
     where, k = "echo_moe_route", fp8.types()
     dev = k.device()
+    if logits.dim() != 2:
+        fp8.refuse(where, f"logits has {logits.dim()} axes")
     T, E, n = logits.shape[0], router.num_experts, router.top_k
+    if T >> 31:
+        fp8.sizes(where, T)
     lp, stride = fp8.rows(where, "logits", logits, (T, E), k.real, dev)
     ip = fp8.address(where, "ids", ids, (T, n), k.i32, dev)
     wp = fp8.address(where, "weights", weights, (T, n), k.f32, dev)
@@ -83,6 +88,7 @@ class Experts:
         if w_down.dim() != 3:
             fp8.refuse(where, f"w_down has {w_down.dim()} axes")
         E, H, I = w_down.shape
+        fp8.sizes(where, E, H, I)
         hb, ib = fp8.blocks(H), fp8.blocks(I)
         self.device = dev = w_down.get_device()
         if dev < 0:
@@ -97,6 +103,7 @@ class Experts:
         self.ref = ctypes.byref(self.c)
 
     def workspace_bytes(self, num_tokens: int, top_k: int) -> int:
+        fp8.sizes("echo_moe_experts_workspace_bytes", num_tokens, top_k)
         n = int(_lib().echo_moe_experts_workspace_bytes(self.ref, int(num_tokens), int(top_k)))
         if n == 0 and echo.last_error():
             raise echo.EchoError(echo.ECHO_E_INVALID, "echo_moe_experts_workspace_bytes",
@@ -112,7 +119,11 @@ def experts(ex: Experts, x, x_scale, ids, weights, out, workspace, residual=None
     dev = k.device()
     if ex.device != dev:
         fp8.refuse(where, f"the experts are on cuda:{ex.device}, the current device is cuda:{dev}")
-    T, H, n = x.shape[0], ex.hidden, ids.shape[-1]
+    if x.dim() != 2 or ids.dim() != 2:
+        fp8.refuse(where, f"x has {x.dim()} axes, ids {ids.dim()}")
+    T, H, n = x.shape[0], ex.hidden, ids.shape[1]
+    if (T | n) >> 31:
+        fp8.sizes(where, T, n)
     xp = fp8.address(where, "x", x, (T, H), k.codes, dev)
     xsp = fp8.address(where, "x_scale", x_scale, (T, -(-H // fp8.BLOCK)), k.f32, dev)
     ip = fp8.address(where, "ids", ids, (T, n), k.i32, dev)
