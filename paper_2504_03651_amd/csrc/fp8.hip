@@ -105,13 +105,14 @@ __device__ __forceinline__ bool plain_block(uint32_t t, float s) {
 }
 
 // Blocks of 1 x 128: 16 lanes a block, 8 values a lane, two blocks at a time; a
-// workgroup has 32 blocks of one row.
+// workgroup has 32 blocks of one row.  first: of the launch's workgroups, in all.
 template <bool F32>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const void *x, int64_t stride, int cols,
                                                             int cb, int parts, uint8_t *codes,
-                                                            float *scales) {
-    const int64_t row = blockIdx.x / parts;
-    const int j0 = 32 * (int)(blockIdx.x - row * parts) + (threadIdx.x >> 4);
+                                                            float *scales, uint32_t first) {
+    const uint32_t b = first + blockIdx.x;
+    const int64_t row = b / parts;
+    const int j0 = 32 * (int)(b - row * parts) + (threadIdx.x >> 4);
     const int lane8 = 8 * (threadIdx.x & 15);
     Eight<F32> v[2];
 #pragma unroll
@@ -143,8 +144,8 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const void *x, int64
 template <bool F32>
 __global__ __launch_bounds__(256) void quantize_blocks_kernel(const void *x, int64_t stride,
                                                               int rows, int cols, int rb, int cb,
-                                                              uint8_t *codes, float *scales) {
-    const int64_t b = blockIdx.x, mr = b / cb;   // matrix and row of blocks
+                                                              uint8_t *codes, float *scales, uint32_t first) {
+    const int64_t b = first + blockIdx.x, mr = b / cb;   // matrix and row of blocks
     const int64_t mat = mr / rb;
     const int j = (int)(b - mr * cb), i = (int)(mr - mat * rb);
     const int col = kQ * j + 8 * (threadIdx.x & 15);
@@ -274,6 +275,7 @@ Cut cut_of(int T, int N, int K) {
         if (!rows_fit(nt, T, K)) continue;
         const int x = rows_tokens(T);
         const int64_t turns = ((int64_t)cdiv(N, 16 * nt) * cdiv(T, x > 16 ? 32 : 16) + 255) / 256;
+        if (turns >= 1 << 15) continue;   // a launch has fewer than 2^32 threads
         const double us = std::max(bytes / 5.2e6, (double)turns * (16 * nt + x) * K / 50e3) + 0.6 +
                           1.5 * (double)(turns - 1);
         if (us < least) least = us, best = Cut{nt == 1 ? kRows16 : kRows32, 1};
@@ -392,22 +394,29 @@ int echo_fp8_quantize(const void *x, int32_t x_dtype, int64_t x_stride, int32_t 
     const int parts = cdiv(cb, 32);   // workgroups of a row
     const int64_t grid = block_rows == 1 ? (int64_t)batch * rows * parts : blocks;
     if (grid > INT32_MAX) return fail(ECHO_E_UNSUPPORTED, "%lld blocks", (long long)blocks);
-    if (block_rows == 1) {
-        if (size == 4)
-            hipLaunchKernelGGL(quantize_rows_kernel<true>, dim3((unsigned)grid), dim3(256), 0, st, x,
-                               x_stride, cols, cb, parts, (uint8_t *)codes, scales);
-        else
-            hipLaunchKernelGGL(quantize_rows_kernel<false>, dim3((unsigned)grid), dim3(256), 0, st, x,
-                               x_stride, cols, cb, parts, (uint8_t *)codes, scales);
-    } else {
-        if (size == 4)
-            hipLaunchKernelGGL(quantize_blocks_kernel<true>, dim3((unsigned)grid), dim3(256), 0, st,
-                               x, x_stride, rows, cols, rb, cb, (uint8_t *)codes, scales);
-        else
-            hipLaunchKernelGGL(quantize_blocks_kernel<false>, dim3((unsigned)grid), dim3(256), 0, st,
-                               x, x_stride, rows, cols, rb, cb, (uint8_t *)codes, scales);
+    // a launch has fewer than 2^32 threads
+    constexpr int64_t kMost = 1 << 23;
+    for (int64_t first = 0; first < grid; first += kMost) {
+        const dim3 groups((unsigned)std::min(kMost, grid - first)), threads(256);
+        if (block_rows == 1) {
+            if (size == 4)
+                hipLaunchKernelGGL(quantize_rows_kernel<true>, groups, threads, 0, st, x, x_stride, cols, cb,
+                                   parts, (uint8_t *)codes, scales, (uint32_t)first);
+            else
+                hipLaunchKernelGGL(quantize_rows_kernel<false>, groups, threads, 0, st, x, x_stride, cols, cb,
+                                   parts, (uint8_t *)codes, scales, (uint32_t)first);
+        } else {
+            if (size == 4)
+                hipLaunchKernelGGL(quantize_blocks_kernel<true>, groups, threads, 0, st, x, x_stride, rows,
+                                   cols, rb, cb, (uint8_t *)codes, scales, (uint32_t)first);
+            else
+                hipLaunchKernelGGL(quantize_blocks_kernel<false>, groups, threads, 0, st, x, x_stride, rows,
+                                   cols, rb, cb, (uint8_t *)codes, scales, (uint32_t)first);
+        }
+        const int rc = launched("echo_fp8_quantize");
+        if (rc) return rc;
     }
-    return launched("echo_fp8_quantize");
+    return ECHO_OK;
 }
 
 size_t echo_fp8_gemm_workspace_bytes(int32_t num_tokens, int32_t out_features,

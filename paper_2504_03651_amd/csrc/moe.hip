@@ -413,7 +413,16 @@ void launch_route(const RouteArgs &a, hipStream_t st) {
 // of 512 experts 8.3 and 12.0 us, 8,000 16.8 and 14.4; of 64 experts 2,000 4.3 and
 // 4.5, 8,000 6.8 and 4.7).
 template <bool F32, bool SIGMOID>
-void launch_route(const RouteArgs &a, hipStream_t st) {
+void launch_route(RouteArgs a, hipStream_t st) {
+    constexpr int kMost = 1 << 25;   // tokens of a launch, which has fewer than 2^32 threads
+    for (; a.T > kMost; a.T -= kMost) {
+        RouteArgs part = a;
+        part.T = kMost;
+        launch_route<F32, SIGMOID>(part, st);
+        a.logits = (const uint8_t *)a.logits + kMost * a.stride * (F32 ? 4 : 2);
+        a.ids += (int64_t)kMost * a.top_k;
+        a.weights += (int64_t)kMost * a.top_k;
+    }
     if (a.T > 4096 && a.top_k < 16 && a.groups <= 16) launch_route<F32, SIGMOID, 16>(a, st);
     else launch_route<F32, SIGMOID, 64>(a, st);
 }
