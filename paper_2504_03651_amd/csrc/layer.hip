@@ -233,6 +233,13 @@ struct Ws {
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
+// A launch has fewer than 2^32 threads: 256 a token, or one for each of its `each` pieces
+int check_threads(int64_t T, int64_t each) {
+    if (T >= 1 << 24 || T * each > ((int64_t)1 << 32) - 256)
+        return fail(ECHO_E_UNSUPPORTED, "%lld tokens are more than a launch holds", (long long)T);
+    return ECHO_OK;
+}
+
 int plan_ws(const echo_layer_t *L, const echo_kv_pool_t *pool, const echo_batch_t *b, Ws *w) {
     if (!L || !pool || !b) return fail(ECHO_E_INVALID, "layer, pool or batch is NULL");
     if (L->hidden <= 0 || L->hidden % 8 || L->intermediate <= 0 || L->intermediate % 8 ||
@@ -251,6 +258,7 @@ int plan_ws(const echo_layer_t *L, const echo_kv_pool_t *pool, const echo_batch_
     const int64_t T = b->num_tokens, H = L->hidden, I = L->intermediate;
     const int64_t qd = (int64_t)L->num_q_heads * L->head_dim;
     const int64_t kd = (int64_t)L->num_kv_heads * L->head_dim;
+    if ((rc = check_threads(T, std::max(qd / 4, I / 8)))) return rc;
     size_t attn_ws = 0;
     if ((rc = echo::attn_bytes(pool, b, L->num_q_heads, &attn_ws, &w->attn_host))) return rc;
     size_t o = 0;
@@ -306,6 +314,7 @@ int plan_moe_ws(const echo_moe_layer_t *L, const echo_kv_pool_t *pool, const ech
     const int64_t qd = (int64_t)L->num_q_heads * L->head_dim;
     const int64_t kd = (int64_t)L->num_kv_heads * L->head_dim;
     if (qd + 2 * kd > INT32_MAX) return fail(ECHO_E_UNSUPPORTED, "%lld columns of qkv", (long long)(qd + 2 * kd));
+    if ((rc = check_threads(T, 0))) return rc;
     size_t attn_ws = 0;
     if ((rc = echo::attn_bytes(pool, b, L->num_q_heads, &attn_ws, &w->attn_host))) return rc;
     // one scratch for the products, the router's library product and the experts

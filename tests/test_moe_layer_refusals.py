@@ -41,3 +41,19 @@ def test_host_workspace_is_checked_before_anything_is_enqueued(name, short):
     rc = getattr(layer._lib(), name)(ctypes.byref(c), ctypes.byref(cp), ctypes.byref(cb), P, P, 1 << 40,
                                      None if short is None else ctypes.addressof(host), short or 0, None)
     assert rc == echo.ECHO_E_WORKSPACE and "host workspace" in echo.last_error(), echo.last_error()
+
+
+@pytest.mark.parametrize("name, tokens, inter", [("moe", 1 << 24, 144), ("dense", 1 << 24, 128), ("dense", 1 << 21, 1 << 14)])
+def test_more_tokens_than_a_launch_holds(name, tokens, inter):
+    """2^32 threads, at 256 a token, or at one for eight activations of the MLP."""
+    layer, c = _moe_layer() if name == "moe" else _dense()
+    if name == "dense":
+        c.intermediate = inter
+    cp, cb, keep = echo.host_structs(W.config1())
+    for f in ("h_block_tables", "h_seq_lens", "h_q_start", "h_row_kind"):
+        setattr(cb, f, None)
+    ask = getattr(layer._lib(), f"echo_{'moe_' if name == 'moe' else ''}layer_workspace_bytes")
+    args = (ctypes.byref(c), ctypes.byref(cp), ctypes.byref(cb))
+    assert ask(*args) > 0
+    cb.num_tokens = tokens
+    assert ask(*args) == 0 and "more than a launch holds" in echo.last_error()
