@@ -403,15 +403,20 @@ void launch_route(const RouteArgs &a, hipStream_t st) {
     const size_t lds = 4 * (size_t)a.E * std::max(8, 4 * U);
     if (a.E <= 64) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, U, LANES>), grid, block, lds, st, a);
     else if (a.E <= 128) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 2 * U, LANES>), grid, block, lds, st, a);
-    else if (a.E <= 256) hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 4 * U, LANES>), grid, block, lds, st, a);
-    else hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 8 * U, LANES>), grid, block, lds, st, a);
+    else if (LANES == 16 || a.E <= 256)
+        hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 4 * U, LANES>), grid, block, lds, st, a);
+    else if constexpr (LANES == 64)
+        hipLaunchKernelGGL((route_kernel<F32, SIGMOID, 8, LANES>), grid, block, lds, st, a);
 }
 
 // Sixteen lanes a token take half the instructions, but four times as long over one
-// token: many tokens go that way, where 16 lanes have a place for each chosen expert
-// and the next, and one for each group (a wave a token, then 16 lanes: 2,000 tokens
-// of 512 experts 8.3 and 12.0 us, 8,000 16.8 and 14.4; of 64 experts 2,000 4.3 and
-// 4.5, 8,000 6.8 and 4.7).
+// token: many tokens of up to 256 experts go that way, where 16 lanes have a place
+// for each chosen expert and the next, and one for each group.  Us by a wave a token
+// and by 16 lanes, 8 chosen, for 2,000, 4,000, 8,000 and 16,000 tokens:
+//    64 experts              4.8 5.3    5.6 5.3    7.7 5.7    11.9 6.9
+//   128, 4 groups            6.8 7.9    8.3 8.1    13.2 11.0  19.0 12.7
+//   256, 8 groups, a bias    11.4 14.9  15.6 18.0  20.8 20.3  29.6 26.6
+//   512                      7.5 11.9   8.9 12.3   14.2 14.9  24.1 31.5
 template <bool F32, bool SIGMOID>
 void launch_route(RouteArgs a, hipStream_t st) {
     constexpr int kMost = 1 << 25;   // tokens of a launch, which has fewer than 2^32 threads
@@ -423,7 +428,7 @@ void launch_route(RouteArgs a, hipStream_t st) {
         a.ids += (int64_t)kMost * a.top_k;
         a.weights += (int64_t)kMost * a.top_k;
     }
-    if (a.T > 4096 && a.top_k < 16 && a.groups <= 16) launch_route<F32, SIGMOID, 16>(a, st);
+    if (a.T > 4096 && a.E <= 256 && a.top_k < 16 && a.groups <= 16) launch_route<F32, SIGMOID, 16>(a, st);
     else launch_route<F32, SIGMOID, 64>(a, st);
 }
 
