@@ -593,11 +593,17 @@ int plan_ws(const echo_experts_t *x, int32_t T, int32_t top_k, Ws *w) {
         return fail(ECHO_E_UNSUPPORTED, "more than 2^32 codes in an expert's matrix (%d x %d) or in x (%d x %d)",
                     2 * x->intermediate, x->hidden, T, x->hidden);
     const int E = x->num_experts;
-    // tiles of as many pairs as experts get on average
-    // (measured either side, 64 experts of 2048 x 1024: 4 pairs an expert, 16 rows
-    // 87 us, 32 rows 87; 8: 101 and 90; 16: 32 rows 108, 64 rows 101; 64: 64 rows
-    // 133, 128 rows 160; 128: 199 and 193)
-    w->tile = R > 96 * (int64_t)E ? 128 : R > 12 * (int64_t)E ? 64 : R > 4 * (int64_t)E ? 32 : 16;
+    // Tiles of as many pairs as experts get on average.  Us with tiles of 16, 32, 64 and
+    // 128 rows, for 64 experts of 2048 x 1024, 128 of 1024 x 512, 16 of 4096 x 4096:
+    //     4 pairs  78 78 -  -       52 52 -  -        183 190  -   -
+    //     8        99 81 83 -       66 55 58 -        213 189 183  -
+    //    16       105 103 88 101    72 68 60 70       221 231 186 218
+    //    64       253 166 127 145   158 107 94 104    478 309 238 233
+    //    80       295 183 156 150   187 121 105 106   584 375 298 275
+    //   128       444 250 197 176   267 168 137 121   882 496 368 287
+    // At 12 pairs tiles of 64 would be up to 11% faster than those of 32, but take their
+    // gate and up sums from e4m3 products (run_experts).
+    w->tile = R > 72 * (int64_t)E ? 128 : R > 12 * (int64_t)E ? 64 : R > 4 * (int64_t)E ? 32 : 16;
     w->max_tiles = (int)(R / w->tile + std::min<int64_t>(E, R));
     if ((int64_t)w->max_tiles * cdiv(x->hidden, 16) > INT32_MAX ||
         (int64_t)w->max_tiles * cdiv(x->intermediate, 16) > INT32_MAX)
