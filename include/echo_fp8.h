@@ -48,9 +48,11 @@ int echo_fp8_quantize(const void *x, int32_t x_dtype, int64_t x_stride, int32_t 
  *           (+ residual[t][n]),
  * x codes [T][K] with scales of 1 x 128, w codes [N][K] (out_features x
  * in_features) with scales of 128 x 128, sums in fp32, y [T][N] bf16 or fp32
- * with rows y_stride >= N elements apart, rounded once (under a bf16 result the
- * e4m3 matrix instructions add 128 products to about 1.5e-5 of the sum; an fp32
- * result takes exact products and fp32 sums).  Scales may be any fp32 numbers: it is
+ * with rows y_stride >= N elements apart, rounded once.  An fp32 result takes
+ * exact products and fp32 sums; under a bf16 result the e4m3 matrix instructions add
+ * products, those of eight neighbours along K cut off towards zero at 2^-13 of the
+ * largest: 1.5e-5 of the sum in the 2-norm where terms are of both signs and alike,
+ * 7 x 2^-13 of the largest of every eight at worst.  Scales may be any fp32 numbers: it is
  * the scaled sum of a block that has to be one, not the product of its scales.
  * residual (optional):
  * of y's type and strides, added before that rounding; it may be y itself, and

@@ -67,8 +67,8 @@ typedef struct {
 /* out[t] = (residual[t] +) sum_j weights[t][j] * expert(ids[t][j])(x[t]):
  * x codes [T][H] with scales of 1 x 128 (echo_fp8_quantize), ids and weights
  * [T][top_k], residual (optional; may be out itself) and out bf16 [T][H].
- * Inside an expert the activation SiLU(gate) * up, in fp32 (of sums as exact as
- * echo_fp8_gemm's under a bf16 result, or better), is requantised in blocks of
+ * Inside an expert the activation SiLU(gate) * up, in fp32 (both products' sums are
+ * as exact as echo_fp8_gemm's under a bf16 result, or better), is requantised in blocks of
  * 1 x 128 as echo_fp8_quantize does (quotients within two ulps); an expert's output
  * is rounded to 11 bits (2^-11 of the value, or 2^-39 of the largest of its 16 or
  * more neighbours) before the weighted sum, which is taken in fp32 in the order of

@@ -22,7 +22,8 @@ namespace fp8 {
 // with a NaN or a scale outside that range take the general form, and no quotient
 // of the others is past 448 by more than a rounding, so nothing needs clamping.  66.5 million
 // bf16 activations take 36 us, 5.6 TB/s (by division, clamped and with 64-bit
-// indices 54), a matrix of 117 million in blocks of 128 x 128 68 (101).
+// indices 54), a matrix of 117 million in blocks of 128 x 128 68 (101); fp32 ones 62
+// and 104 us, 5.4 and 5.6 TB/s.
 
 // Eight values as they lie in memory
 template <bool F32>
@@ -258,14 +259,17 @@ size_t most_parts_bytes(int T, int N, int K) {
     return std::min<size_t>((size_t)rows * pitch_of(N) * 4, kPartBytes);
 }
 
-// The cut of least estimated time, in microseconds fitted to 130 sizes (T 1 to
-// 4,640, N x K from 512 x 512 to 28672 x 4096, weights from memory).
+// The cut of least estimated time, in microseconds fitted to bf16 results of 130 sizes
+// (T 1 to 4,640, N x K from 512 x 512 to 28672 x 4096, weights from memory).  Over 144
+// sizes of today's kernels it is 1.6% (geometric mean) above the best cut of each,
+// 29% at most (80 to 96 x 4096 x 4096, where rows would be best), over 60 with fp32
+// results 2.8% and 34%.
 //   Weights and tokens come at 5.2 TB/s at most.
 //   kRows: 16 or 32 weight rows a workgroup, every wave on its own; one workgroup a
-//   CU, which takes in 50 KB a microsecond, tokens among them (8 x 6144 x 4096: 9.0
-//   by 32 rows, 11.0 by 16; 8 x 4096 x 4096: 8.0 and 7.2).
+//   CU, which takes in 50 KB a microsecond, tokens among them (8 x 6144 x 4096: 8.5
+//   by 32 rows, 11.1 by 16; 8 x 4096 x 4096: 8.1 and 7.4).
 //   Ranges of K cost a second launch and their fp32 parts' way to memory and back
-//   (137 x 4096 x 14336: 95 in one range, 30.7 to 32 in eight).
+//   (137 x 4096 x 14336: 125 in one range, 33 in eight, 41 in sixteen).
 Cut cut_of(int T, int N, int K) {
     const int KB = cdiv(K, kQ);
     const double bytes = (double)N * K + (double)T * K;
@@ -325,9 +329,8 @@ hipError_t launch_gemm(const ProductArgs &p, Cut c, hipStream_t st) {
         case k64x64: e = launch_tiles<F32, 64, 64, 4, 1, 4>(p, c.splits, st); break;
         default:
             // fp32 results, which widen every operand that a wave reads, in waves of
-            // 64 x 64, two workgroups a CU (4,640 x 4096 x 4096: 172 us; in tiles of 128
-            // x 64 with waves of 32 x 64 245, and 1,024 x 6144 x 4096 74 and 75, in
-            // tiles of 128 x 128 with such waves 90)
+            // 64 x 64, two workgroups a CU (4,640 x 4096 x 4096: 178 us, in tiles of 128 x
+            // 64 with waves of 32 x 64 214; 1,024 x 6144 x 4096 69 and 66)
             if (c.form == k128x64) e = launch_tiles<F32, 128, 64, 4, 1, 3>(p, c.splits, st);
             else if (F32) e = launch_tiles<true, 128, 128, 2, 2, 2>(p, c.splits, st);
             else if (c.form == k128x128) e = launch_tiles<false, 128, 128, 4, 2, 4>(p, c.splits, st);

@@ -198,10 +198,13 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
 // each of its tokens, and one (GateUp: two) of its weight rows.  Each step's sum
 // comes out of the matrix instruction alone and is scaled on its way into the
 // accumulators, one FMA a value.
-// Bound by LDS: a step of 256 x 256 copies 64 KB in and its waves of 128 x 64 (the
-// largest whose sums fit the registers that FMAs reach) read 192 KB, 1.8 us at the
-// 142 bytes a nanosecond that a CU reads; it takes 1.9, the matrix instructions in it
-// 1.0: 4,640 x 28672 x 4096 in 609 us, 1.79 PFLOP/s.  A step of 256 x 128 takes 1.3.
+// Bound by the copies into LDS: 4,640 x 28672 x 4096 takes 600 us, 1.82 PFLOP/s, its
+// copies alone 484 (9.2 TB/s over all CUs), all the rest without them 407; 137 x 4096 x
+// 14336 34, 32 and 29; 4,640 tokens through 64 experts of 2048 x 1024 497, 401 and 387.
+// A step of 256 x 256 copies 64 KB in 1.9 us, one of 256 x 128 48 KB in 1.3.  Matrix
+// instructions are busy 39% of the first one's time, vector instructions 35%, LDS 18%,
+// with no conflicts in the steps.  Waves of 128 x 64 are the largest whose sums fit
+// the registers that FMAs reach.
 // No more workgroups are launched than run at once: each goes on to a next tile,
 // whose first copies it starts before it writes the last one's results (4,640 tokens
 // through 64 experts 510 -> 498 us).
