@@ -65,8 +65,9 @@ __device__ __forceinline__ uint32_t scale_class(float s) {   // below kOddClass:
 }
 __device__ __forceinline__ bool odd_scale(float s) { return scale_class(s) < kOddClass; }
 __device__ __forceinline__ f32x4 scaled(f32x4 v, float x, float w) {
-    const bool x_less = fabsf(x) < fabsf(w), small = fabsf(x * w) < 1.f;
+    const bool x_less = fabsf(x) < fabsf(w);
     const float less = x_less ? x : w, more = x_less ? w : x;
+    const bool small = fabsf(x * w) < 1.f && less != 0.f;   // 0 first: it leaves no infinity
     return v * (small ? more : less) * (small ? less : more);
 }
 

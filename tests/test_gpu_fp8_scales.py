@@ -72,6 +72,21 @@ def test_gemm_scales_whose_product_is_infinite(T, N, K, f32):
     _bounded(_gemm(x, xs, w, ws, f32), want, S, K, f32)
 
 
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("T, N, K", SHAPES)
+def test_gemm_scales_of_zero_beside_the_largest(T, N, K, f32):
+    """A block under a scale of zero adds nothing, whatever the other scale and the
+    block's sum: tokens of 2^120 and one of 2^-149 by rows of zero and ordinary ones."""
+    g = np.random.default_rng(T * N + K)
+    x, xs = activations(g, T, K)
+    w, ws = weights(g, N, K)
+    xs[::2, 0] = 2.0 ** 120
+    xs[1, 0] = 2.0 ** -149
+    ws[:, 0] = 0
+    want, S = FO.gemm(x, xs, w, ws)
+    _bounded(_gemm(x, xs, w, ws, f32), want, S, K, f32)
+
+
 @pytest.mark.parametrize("gate, up, down", [(2.0 ** 40, 2.0 ** -77, 2.0 ** 60), (1.0, 2.0 ** -60, 2.0 ** -56)])
 @pytest.mark.parametrize("T", [3, 50, 100, 700])
 def test_experts_scales_whose_product_is_subnormal(T, gate, up, down):
