@@ -207,10 +207,10 @@ __device__ __forceinline__ void finish(const ProductArgs &p, uint8_t *lds,
 // the registers that FMAs reach.
 // No more workgroups are launched than run at once: each goes on to a next tile,
 // whose first copies it starts before it writes the last one's results (4,640 tokens
-// through 64 experts 510 -> 498 us).
+// through 64 experts 509 -> 497 us).
 // ONCE: weights past the caches, where one tile of tokens reads them (8 tokens
-// through 64 experts of 2048 x 1024 66.6 -> 61.5 us, 64 tokens 92 -> 83; 64 x 28672
-// x 4096 35.8 -> 33.4; but two tiles of 64, 100 x 4096 x 4096: 15.5 -> 16.3).
+// through 64 experts of 2048 x 1024 65.7 -> 60.2 us, 64 tokens 93 -> 84; 64 x 28672
+// x 4096 35.2 -> 33; but two tiles of 64, 100 x 4096 x 4096: 15.5 -> 16.3).
 // F32: products are exact (mfma128), and Plain's results fp32.
 // part: fp32 sums of one of `splits` equal ranges of K go to part[split][t][n],
 // rows part_pitch apart, instead of y.
