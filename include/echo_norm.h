@@ -37,7 +37,7 @@ typedef enum { ECHO_NORM_NONE = 0, ECHO_NORM_RMS = 1, ECHO_NORM_LAYER = 2 } echo
 enum { ECHO_I8 = 2 };
 
 typedef struct {
-    int32_t hidden;        /* H, 1 to 32768 */
+    int32_t hidden;        /* H, 1 to 32768 (codes: to 16384) */
     int32_t post, pre;     /* echo_norm_kind_t */
     int32_t param_dtype;   /* ECHO_BF16 or ECHO_F32: of weights and biases [H] */
     float post_eps, pre_eps;

@@ -32,88 +32,106 @@ struct Args {
     const uint8_t *post_w, *post_b, *pre_w, *pre_b;
     int H, post, pre, param_f32;
     float post_eps, pre_eps, residual_scale, block_scale, weight_offset;
-    int rows;
+    double inv_h;   // 1 / H
+    int rows, in_place;
 };
 
-// Eight neighbouring values at any alignment of an element, n of which are there
+// Eight neighbouring values as they lie in memory, at any alignment of an element.
+// BF: all tensors and parameters of the call are bf16.  TINY: rows shorter than eight,
+// of which n are there.
+template <bool BF, bool TINY>
 struct Raw {
-    u32x4 a, b;
+    u32x4 a[BF ? 1 : 2];
     __device__ __forceinline__ void load(const uint8_t *p, int f32, int64_t at, int n) {
-        if (f32) {
+        if (!BF && f32) {
             const float *q = (const float *)p + at;
-            if (n >= 8) {
-                a = __builtin_bit_cast(u32x4, *(const any_f32x4 *)q);
-                b = __builtin_bit_cast(u32x4, *(const any_f32x4 *)(q + 4));
-            } else {
+            if constexpr (TINY) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    a[i] = i < n ? __float_as_uint(q[i]) : 0u;
-                    b[i] = i + 4 < n ? __float_as_uint(q[i + 4]) : 0u;
-                }
+                for (int i = 0; i < 8; ++i) a[BF ? 0 : i / 4][i % 4] = i < n ? __float_as_uint(q[i]) : 0u;
+            } else {
+                a[0] = __builtin_bit_cast(u32x4, *(const any_f32x4 *)q);
+                a[BF ? 0 : 1] = __builtin_bit_cast(u32x4, *(const any_f32x4 *)(q + 4));
             }
         } else {
             const uint16_t *q = (const uint16_t *)p + at;
-            if (n >= 8) {
-                a = *(const any_u32x4 *)q;
-            } else {
+            if constexpr (TINY) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    a[i] = (2 * i < n ? q[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)q[2 * i + 1] << 16 : 0u);
+                    a[0][i] = (2 * i < n ? q[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)q[2 * i + 1] << 16 : 0u);
+            } else {
+                a[0] = *(const any_u32x4 *)q;
             }
         }
     }
-    __device__ __forceinline__ void get(int f32, float (&v)[8]) const {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t wide = i < 4 ? a[i % 4] : b[i % 4];
-            const uint32_t half = i & 1 ? a[i / 2] & 0xFFFF0000u : a[i / 2] << 16;
-            v[i] = __uint_as_float(f32 ? wide : half);
-        }
+    __device__ __forceinline__ float get(int f32, int i) const {
+        const uint32_t half = i & 1 ? a[0][i / 2] & 0xFFFF0000u : a[0][i / 2] << 16;
+        if constexpr (BF) return __uint_as_float(half);
+        return __uint_as_float(f32 ? a[BF ? 0 : i / 4][i % 4] : half);
     }
 };
 
-// n of eight values to a row of bf16 or fp32
+template <bool BF, bool TINY>
 __device__ __forceinline__ void store8(uint8_t *p, int f32, int64_t at, int n, const float (&v)[8]) {
-    if (f32) {
+    if (!BF && f32) {
         float *q = (float *)p + at;
-        if (n >= 8) {
+        if constexpr (TINY) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) q[i] = v[i];
+        } else {
             *(any_f32x4 *)q = (f32x4){v[0], v[1], v[2], v[3]};
             *(any_f32x4 *)(q + 4) = (f32x4){v[4], v[5], v[6], v[7]};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 7; ++i)
-                if (i < n) q[i] = v[i];
         }
     } else {
         uint16_t *q = (uint16_t *)p + at;
-        if (n >= 8) {
-            *(any_u32x4 *)q = (u32x4){f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7])};
-        } else {
+        if constexpr (TINY) {
 #pragma unroll
-            for (int i = 0; i < 7; ++i)
+            for (int i = 0; i < 8; ++i)
                 if (i < n) q[i] = (uint16_t)f2bf(v[i]);
+        } else {
+            *(any_u32x4 *)q = (u32x4){f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7])};
         }
     }
 }
 
-// Sums and maxima over a row's WAVES waves.  `room` alternates between two places, so
-// that one barrier a call is enough.
+// Sums and maxima over a row's WAVES waves, a barrier each: the lanes of sixteen meet
+// by DPP, the rest in LDS, in places that take turns.
+template <int CTRL>
+__device__ __forceinline__ float turned(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
+}
+template <int CTRL>
+__device__ __forceinline__ double turned(double v) {
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xF, 0xF, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xF, 0xF, false);
+    return __hiloint2double(hi, lo);
+}
+
 template <typename T, int WAVES>
 struct Across {
-    T (*room)[WAVES];
+    static constexpr bool kWide = WAVES > 4;   // waves meet first
+    static constexpr int kParts = WAVES == 1 ? 1 : kWide ? WAVES : 4 * WAVES;
+    T (*room)[kParts];
     int turn;
     template <typename F>
     __device__ __forceinline__ T all(T v, F join) {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) v = join(v, __shfl_xor(v, o));
+        v = join(v, turned<0x128>(v));   // row_ror:8, 4, 2, 1
+        v = join(v, turned<0x124>(v));
+        v = join(v, turned<0x122>(v));
+        v = join(v, turned<0x121>(v));
+        if constexpr (WAVES == 1 || kWide) {
+            v = join(v, __shfl_xor(v, 16));
+            v = join(v, __shfl_xor(v, 32));
+        }
         if constexpr (WAVES > 1) {
             T *part = room[turn];
             turn ^= 1;
-            if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+            constexpr int LANES = kWide ? 64 : 16;
+            if (threadIdx.x % LANES == 0) part[threadIdx.x / LANES] = v;
             __syncthreads();
             v = part[0];
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) v = join(v, part[w]);
+            for (int w = 1; w < kParts; ++w) v = join(v, part[w]);
         }
         return v;
     }
@@ -125,185 +143,264 @@ struct Across {
     }
 };
 
-__device__ __forceinline__ float root(float x) { return sqrtf(x); }
-__device__ __forceinline__ double root(double x) { return sqrt(x); }
-
-// x -> its norm: mean and squares by sums over the row, then weight and bias
-template <typename T, int V, int LANES, typename S>
-__device__ __forceinline__ void normed(const Args &a, int kind, const uint8_t *w, const uint8_t *b, float eps,
-                                       int lane, S &across, T (&x)[V][8]) {
-    if (kind == ECHO_NORM_NONE) return;
-    // (sums are divided by H: a row of one value has exactly that for its mean)
-    T mean = T(0);
-    if (kind == ECHO_NORM_LAYER) {
-        T s = T(0);
-#pragma unroll
-        for (int u = 0; u < V; ++u)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s += x[u][i];   // 0 past the row's end
-        mean = across.sum(s) / (T)a.H;
-#pragma unroll
-        for (int u = 0; u < V; ++u)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                x[u][i] = 8 * (lane + LANES * u) + i < a.H ? x[u][i] - mean : T(0);
-    }
-    T ss = T(0);
-#pragma unroll
-    for (int u = 0; u < V; ++u)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) ss += x[u][i] * x[u][i];
-    const T inv = T(1) / root(across.sum(ss) / (T)a.H + (T)eps);
-#pragma unroll
-    for (int u = 0; u < V; ++u) {
-        const int col = 8 * (lane + LANES * u), n = a.H - col;
-        if (n <= 0) continue;
-        Raw r;
-        float f[8];
-        if (w) {
-            r.load(w, a.param_f32, col, n);
-            r.get(a.param_f32, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] *= inv * ((T)f[i] + (T)a.weight_offset);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] *= inv;
-        }
-        if (b) {
-            r.load(b, a.param_f32, col, n);
-            r.get(a.param_f32, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] += (T)f[i];
-        }
-    }
+__device__ __forceinline__ float inverse_root(float x) { return rsqrtf(x); }
+// v_rsq_f64 is good to 2^-24 and better; one step of third order leaves 2^-70 of that
+__device__ __forceinline__ double inverse_root(double x) {
+    const double y = __builtin_amdgcn_rsq(x), e = __builtin_fma(-x * y, y, 1.0);
+    return __builtin_fma(y * e, __builtin_fma(e, 0.375, 0.5), y);
 }
 
 // A row for WAVES waves (1: four rows a workgroup), V times eight values a lane, held
 // in registers from the first step to the last.  T: what sums and rows are held in.
-template <typename T, int WAVES, int V>
+// The last eight of a row begin at H - 8, whatever H is a multiple of: what a lane
+// before them has too counts for that one alone (`skip`), and comes out the same, to be
+// written twice.  Where V <= 2 every input is asked for before the first sum.
+template <typename T, int WAVES, int V, bool BF, bool TINY>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Args a, uint32_t first) {
     constexpr int LANES = 64 * WAVES;
-    __shared__ T room[2][WAVES];
+    constexpr bool EARLY = V <= 2;
+    typedef Raw<BF, TINY> R;
+    __shared__ __align__(16) T room[2][Across<T, WAVES>::kParts];
     Across<T, WAVES> across{room, 0};
     const int lane = threadIdx.x % LANES;
-    const int64_t row = WAVES == 1 ? 4 * ((int64_t)first + blockIdx.x) + threadIdx.x / 64 : (int64_t)first + blockIdx.x;
-    if (WAVES == 1 && row >= a.rows) return;
-    T x[V][8];
-    auto column = [&](int u) { return 8 * (lane + LANES * u); };
-#pragma unroll
-    for (int u = 0; u < V; ++u)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[u][i] = T(0);
-    if (a.block.data) {
-#pragma unroll
-        for (int u = 0; u < V; ++u) {
-            const int n = a.H - column(u);
-            if (n <= 0) continue;
-            Raw r;
-            float f[8];
-            r.load(a.block.data, a.block.f32, row * a.block.stride + column(u), n);
-            r.get(a.block.f32, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = (T)f[i];
-        }
-        normed<T, V, LANES>(a, a.post, a.post_w, a.post_b, a.post_eps, lane, across, x);
+    int64_t row = WAVES == 1 ? 4 * ((int64_t)first + blockIdx.x) + threadIdx.x / 64 : (int64_t)first + blockIdx.x;
+    if (WAVES == 1) {
+        if (row >= a.rows) return;
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)row);   // a wave has one
+        row = (int64_t)((uint64_t)row >> 32 << 32 | lo);
     }
+    int col[V], skip[V];   // the first column of a unit, its values that are another's
 #pragma unroll
     for (int u = 0; u < V; ++u) {
-        const int col = column(u), n = a.H - col;
-        if (n <= 0) continue;
-        Raw r;
-        float f[8];
-        if (a.block.data) {
-            if (a.gate.data) {
-                r.load(a.gate.data, a.gate.f32, row * a.gate.stride + col, n);
-                r.get(a.gate.f32, f);
+        const int at = 8 * (lane + LANES * u);
+        col[u] = TINY ? 0 : min(at, a.H - 8);
+        skip[u] = TINY ? (at ? 8 : 0) : min(at - col[u], 8);
+    }
+    const int n = TINY ? a.H : 8;
+    auto mine = [&](int u, int i) { return i >= skip[u] && (!TINY || i < a.H); };
+    auto take = [&](const Rows &r, int u) {
+        R v;
+        v.load(r.data, r.f32, row * r.stride + col[u], n);
+        return v;
+    };
+    auto param = [&](const uint8_t *p, int u) {
+        R v;
+        v.load(p, a.param_f32, col[u], n);
+        return v;
+    };
+    const bool block = a.block.data, gate = block && a.gate.data, residual = a.residual.data, y = a.y.data;
+    R rb[EARLY ? V : 1], rg[EARLY ? V : 1], rr[EARLY ? V : 1], rw[EARLY ? V : 1], rw2[EARLY ? V : 1];
+    if constexpr (EARLY) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[u][i] *= (T)f[i];
-            }
+        for (int u = 0; u < V; ++u)
+            if (block) rb[u] = take(a.block, u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] *= (T)a.block_scale;
-        }
-        if (a.residual.data) {
-            r.load(a.residual.data, a.residual.f32, row * a.residual.stride + col, n);
-            r.get(a.residual.f32, f);
-            if (a.block.data) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[u][i] += (T)a.residual_scale * (T)f[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[u][i] = (T)a.residual_scale * (T)f[i];
-            }
-        }
-        // past the row's end all is 0, whatever the gate's and norm's zeros met
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[u][i] = i < n ? x[u][i] : T(0);
-        if (a.sum.data) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = (float)x[u][i];
-            store8(a.sum.data, a.sum.f32, row * a.sum.stride + col, n, f);
+        for (int u = 0; u < V; ++u) {
+            if (residual) rr[u] = take(a.residual, u);
+            if (gate) rg[u] = take(a.gate, u);
+            if (a.post_w) rw[u] = param(a.post_w, u);
+            if (a.pre_w) rw2[u] = param(a.pre_w, u);
         }
     }
-    if (!a.y.data) return;
-    normed<T, V, LANES>(a, a.pre, a.pre_w, a.pre_b, a.pre_eps, lane, across, x);
+    auto apart = [] {   // loads of the next unit wait for this one's registers
+        if constexpr (!EARLY) __builtin_amdgcn_sched_barrier(0);
+    };
+
+    T x[V][8];
+    // x less its mean (LAYER) and 1 / sqrt(mean of squares + eps).  The sum is divided by H
+    // exactly enough that a row of one value has that for its mean.
+    auto inverse = [&](int kind, float eps) {
+        if (kind == ECHO_NORM_LAYER) {
+            T s = T(0);
+#pragma unroll
+            for (int u = 0; u < V; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s += mine(u, i) ? x[u][i] : T(0);
+            s = across.sum(s);
+            const T by = (T)a.inv_h;
+            T mean = s * by;
+            mean = fma(fma(-mean, (T)a.H, s), by, mean);
+#pragma unroll
+            for (int u = 0; u < V; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[u][i] -= mean;
+        }
+        T ss = T(0);
+#pragma unroll
+        for (int u = 0; u < V; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss = fma(x[u][i], mine(u, i) ? x[u][i] : T(0), ss);
+        return inverse_root(fma(across.sum(ss), (T)a.inv_h, (T)eps));
+    };
+    const T offset = (T)a.weight_offset;
+    if (block) {
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+            apart();
+            const R r = EARLY ? rb[EARLY ? u : 0] : take(a.block, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[u][i] = (T)r.get(a.block.f32, i);
+        }
+        T by = (T)a.block_scale;
+        if (a.post != ECHO_NORM_NONE) {
+            const T inv = inverse(a.post, a.post_eps);
+            if (a.post_w) {
+#pragma unroll
+                for (int u = 0; u < V; ++u) {
+                    apart();
+                    const R w = EARLY ? rw[EARLY ? u : 0] : param(a.post_w, u);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[u][i] *= (T)w.get(a.param_f32, i) + offset;
+                }
+            }
+            if (a.post_b) {
+#pragma unroll
+                for (int u = 0; u < V; ++u) {
+                    apart();
+                    const R w = param(a.post_b, u);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[u][i] = fma(x[u][i], inv, (T)w.get(a.param_f32, i));
+                }
+            } else {
+                by *= inv;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < V; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[u][i] *= by;
+        if (gate) {
+#pragma unroll
+            for (int u = 0; u < V; ++u) {
+                apart();
+                const R g = EARLY ? rg[EARLY ? u : 0] : take(a.gate, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[u][i] *= (T)g.get(a.gate.f32, i);
+            }
+        }
+    }
+    if (residual) {
+        const T by = (T)a.residual_scale;
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+            apart();
+            const R r = EARLY ? rr[EARLY ? u : 0] : take(a.residual, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const T f = (T)r.get(a.residual.f32, i);
+                x[u][i] = block ? fma(f, by, x[u][i]) : f * by;
+            }
+        }
+    }
+    // In place, a lane's last eight may be another's too: all have read theirs.
+    if (WAVES > 1 && a.in_place) __syncthreads();
+    if (a.sum.data) {
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+            apart();
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = (float)x[u][i];
+            if (skip[u] < 8) store8<BF, TINY>(a.sum.data, a.sum.f32, row * a.sum.stride + col[u], n, f);
+        }
+    }
+    if (!y) return;
+    T inv = T(1);
+    if (a.pre != ECHO_NORM_NONE) {
+        inv = inverse(a.pre, a.pre_eps);
+        if (a.pre_w) {
+#pragma unroll
+            for (int u = 0; u < V; ++u) {
+                apart();
+                const R w = EARLY ? rw2[EARLY ? u : 0] : param(a.pre_w, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[u][i] *= (T)w.get(a.param_f32, i) + offset;
+            }
+        }
+        if (a.pre_b) {
+#pragma unroll
+            for (int u = 0; u < V; ++u) {
+                apart();
+                const R w = param(a.pre_b, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[u][i] = fma(x[u][i], inv, (T)w.get(a.param_f32, i));
+            }
+            inv = T(1);
+        }
+    }
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int u = 0; u < V; ++u) {
-            const int n = a.H - column(u);
-            if (n > 0) store8(a.y.data, a.y.f32, row * a.y.stride + column(u), n, x[u]);
+            apart();
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = x[u][i] * inv;
+            if (skip[u] < 8) store8<BF, TINY>(a.y.data, a.y.f32, row * a.y.stride + col[u], n, f);
         }
     } else {
+        // y is x inv; the largest of one is the largest of the other's
         T top = T(0);
+        bool nan = false;
 #pragma unroll
         for (int u = 0; u < V; ++u)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const T m = fabs(x[u][i]);
-                top = fmax(top, i < a.H - column(u) ? (m != m ? (T)INFINITY : m) : T(0));
+                if (TINY && !mine(u, i)) continue;
+                top = fmax(top, fabs(x[u][i]));
+                nan |= x[u][i] != x[u][i];
             }
-        top = across.max(top);
+        top = across.max(nan ? (T)INFINITY : top) * inv;
         float s = (float)(top / T(127));
         if (s == 0.f) s = 1.f;
         const bool odd = !(s < INFINITY);
         if (odd) s = __uint_as_float(0x7FC00000u);
         if (lane == 0) a.y_scale[row] = s;
-        const T by = T(1) / (T)s;
+        const T by = T(1) / (T)s, both = by * inv;
+        // a quotient corrected by its residual is exact where it is a tie, as those of sums
+        // that no norm has touched may be; scales that are hardly numbers leave some past 127
+        const bool plain = a.pre != ECHO_NORM_NONE && s >= 0x1p-100f;
 #pragma unroll
         for (int u = 0; u < V; ++u) {
-            const int col = column(u), n = a.H - col;
-            if (n <= 0) continue;
+            apart();
             uint32_t q[2] = {0u, 0u};
             if (!odd) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    // the quotient, corrected by its residual: exact where it is a tie
-                    T v = x[u][i] * by;
-                    v = fma(fma(-v, (T)s, x[u][i]), by, v);
-                    v = v > T(127) ? T(127) : v < T(-127) ? T(-127) : v;
-                    // the nearest integer (ties to even) in the low bits
-                    const uint32_t code = (uint32_t)__double_as_longlong(v + 6755399441055744.0) & 0xFFu;
-                    q[i / 4] |= code << (8 * (i % 4));
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t c[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const T f = x[u][4 * h + i];
+                        T v = f * both;
+                        if (!plain) {
+                            v = fma(fma(-v, (T)s, f * inv), by, v);
+                            v = fmin(fmax(v, T(-127)), T(127));
+                        }
+                        // the nearest integer (ties to even) in the low bits
+                        c[i] = (uint32_t)__double2loint(v + 6755399441055744.0);
+                    }
+                    q[h] = __builtin_amdgcn_perm(c[1], c[0], 0x0C0C0400u) | __builtin_amdgcn_perm(c[3], c[2], 0x04000C0Cu);
                 }
             }
-            uint8_t *to = a.y.data + row * a.y.stride + col;
-            if (n >= 8) {
+            uint8_t *to = a.y.data + row * a.y.stride + col[u];
+            if (skip[u] == 8) continue;
+            if constexpr (TINY) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < n) to[i] = (uint8_t)(q[i / 4] >> (8 * (i % 4)));
+            } else {
                 typedef uint32_t pair __attribute__((ext_vector_type(2), aligned(1)));
                 *(pair *)to = (pair){q[0], q[1]};
-            } else {
-#pragma unroll
-                for (int i = 0; i < 7; ++i)
-                    if (i < n) to[i] = (uint8_t)(q[i / 4] >> (8 * (i % 4)));
             }
         }
     }
 }
 
-template <typename T, int WAVES, int V>
+template <typename T, int WAVES, int V, bool BF, bool TINY = false>
 hipError_t launch(const Args &a, hipStream_t st) {
     constexpr int64_t kMost = 1 << 22;   // a launch has fewer than 2^32 threads
     const int64_t grid = WAVES == 1 ? ((int64_t)a.rows + 3) / 4 : a.rows;
     for (int64_t first = 0; first < grid; first += kMost) {
-        hipLaunchKernelGGL((join_kernel<T, WAVES, V>), dim3((unsigned)std::min(kMost, grid - first)),
+        hipLaunchKernelGGL((join_kernel<T, WAVES, V, BF, TINY>), dim3((unsigned)std::min(kMost, grid - first)),
                            dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, st, a, (uint32_t)first);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -311,14 +408,16 @@ hipError_t launch(const Args &a, hipStream_t st) {
     return hipSuccess;
 }
 
-template <typename T>
+template <typename T, bool BF>
 hipError_t launch_by_width(const Args &a, hipStream_t st) {
-    if (a.H <= 512) return launch<T, 1, 1>(a, st);
-    if (a.H <= 2048) return launch<T, 4, 1>(a, st);
-    if (a.H <= 4096) return launch<T, 4, 2>(a, st);
-    if (a.H <= 8192) return launch<T, 8, 2>(a, st);
-    if (a.H <= 16384) return launch<T, 8, 4>(a, st);
-    return launch<T, 8, 8>(a, st);
+    if (a.H < 8) return launch<T, 1, 1, false, true>(a, st);
+    if (a.H <= 512) return launch<T, 1, 1, BF>(a, st);
+    if (a.H <= 2048) return launch<T, 4, 1, BF>(a, st);
+    if (a.H <= 4096) return launch<T, 8, 1, BF>(a, st);
+    if (a.H <= 8192) return launch<T, 8, 2, BF>(a, st);
+    if (a.H <= 16384) return launch<T, 8, 4, BF>(a, st);
+    if constexpr (sizeof(T) == 4) return launch<T, 16, 4, BF>(a, st);
+    return hipErrorInvalidValue;   // codes: refused above
 }
 
 // rows of a tensor that a call names, checked; `codes`: int8 ones are allowed
@@ -390,6 +489,7 @@ int echo_norm_join(const echo_norm_t *norm, int32_t num_tokens, const echo_rows_
         if (q.out.data && q.out.data == q.in.data && (!q.same_type || q.out.stride != q.in.stride))
             return fail(ECHO_E_INVALID, "%s of another type or stride, or may not be", q.what);
     const bool codes = a.y.data && y->dtype == ECHO_I8;
+    if (codes && H > 16384) return fail(ECHO_E_UNSUPPORTED, "hidden %d above 16384 for codes", H);
     if (codes && !y_scale) return fail(ECHO_E_INVALID, "y_scale is NULL");
     if (codes && (uintptr_t)y_scale & 3u) return fail(ECHO_E_INVALID, "y_scale must be 4-byte aligned");
     a.y_scale = codes ? y_scale : nullptr;
@@ -400,6 +500,8 @@ int echo_norm_join(const echo_norm_t *norm, int32_t num_tokens, const echo_rows_
     a.H = H;
     a.post = norm->post;
     a.pre = norm->pre;
+    if (a.post == ECHO_NORM_NONE) a.post_w = a.post_b = nullptr;
+    if (a.pre == ECHO_NORM_NONE) a.pre_w = a.pre_b = nullptr;
     a.param_f32 = norm->param_dtype == ECHO_F32;
     a.post_eps = norm->post_eps;
     a.pre_eps = norm->pre_eps;
@@ -407,8 +509,14 @@ int echo_norm_join(const echo_norm_t *norm, int32_t num_tokens, const echo_rows_
     a.block_scale = norm->block_scale;
     a.weight_offset = norm->weight_offset;
     a.rows = num_tokens;
-    const hipError_t e = codes ? launch_by_width<double>(a, (hipStream_t)stream)
-                               : launch_by_width<float>(a, (hipStream_t)stream);
+    a.inv_h = 1.0 / H;
+    for (const Rows &out : {a.sum, a.y})
+        a.in_place |= out.data && (out.data == a.block.data || out.data == a.residual.data);
+    bool bf = !a.param_f32;
+    for (const Rows &r : {a.block, a.gate, a.residual, a.sum, a.y}) bf &= !r.f32;
+    const hipStream_t st = (hipStream_t)stream;
+    const hipError_t e = codes ? (bf ? launch_by_width<double, true>(a, st) : launch_by_width<double, false>(a, st))
+                               : (bf ? launch_by_width<float, true>(a, st) : launch_by_width<float, false>(a, st));
     return e == hipSuccess ? ECHO_OK : fail(ECHO_E_HIP, "echo_norm_join: %s", hipGetErrorString(e));
 }
 

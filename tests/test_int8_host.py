@@ -199,7 +199,8 @@ def _join(change, rows, T=4, scale=P):
 
 
 @pytest.mark.parametrize("change, rows, code, what", [
-    (dict(hidden=0), {}, INV, "hidden"), (dict(hidden=32769), {}, UNS, "hidden"), (dict(post=3), {}, UNS, "norm"),
+    (dict(hidden=0), {}, INV, "hidden"), (dict(hidden=32769), {}, UNS, "hidden"),
+    (dict(hidden=16385), {n: (v[0], v[1], 16385) for n, v in ROWS.items() if v}, UNS, "hidden"), (dict(post=3), {}, UNS, "norm"),
     (dict(pre=-1), {}, UNS, "norm"), (dict(param_dtype=2), {}, UNS, "dtype"), (dict(post_eps=-1.0), {}, INV, "eps"),
     (dict(pre_eps=float("nan")), {}, INV, "eps"), (dict(residual_scale=float("inf")), {}, INV, "scale"),
     (dict(weight_offset=float("nan")), {}, INV, "weight_offset"), (dict(pre_bias=at(1)), {}, INV, "alignment"),
