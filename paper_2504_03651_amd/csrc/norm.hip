@@ -20,6 +20,8 @@ using fp8::f32x4;
 using fp8::u32x2;
 using fp8::u32x4;
 
+constexpr int kFewRows = 512;
+
 struct Rows {
     uint8_t *data;   // null: there is none
     int64_t stride;  // elements
@@ -36,9 +38,11 @@ struct Args {
     int rows, in_place;
 };
 
+// Rows of whole eights, of any other width, and those shorter than eight
+enum class Width { Whole, Odd, Tiny };
+
 // Eight neighbouring values as they lie in memory, at any alignment of an element.
-// BF: all tensors and parameters of the call are bf16.  TINY: rows shorter than eight,
-// of which n are there.
+// BF: all tensors and parameters of the call are bf16.  TINY: n of them are there.
 template <bool BF, bool TINY>
 struct Raw {
     u32x4 a[BF ? 1 : 2];
@@ -154,11 +158,11 @@ __device__ __forceinline__ double inverse_root(double x) {
 // in registers from the first step to the last.  T: what sums and rows are held in.
 // The last eight of a row begin at H - 8, whatever H is a multiple of: what a lane
 // before them has too counts for that one alone (`skip`), and comes out the same, to be
-// written twice.  Where V <= 2 every input is asked for before the first sum.
-template <typename T, int WAVES, int V, bool BF, bool TINY>
+// written twice.  In rows of whole eights lanes behind the end hold zeros.  Where V <= 2 every input is asked for before the first sum.
+template <typename T, int WAVES, int V, bool BF, Width W>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Args a, uint32_t first) {
     constexpr int LANES = 64 * WAVES;
-    constexpr bool EARLY = V <= 2;
+    constexpr bool EARLY = V <= 2, TINY = W == Width::Tiny, WHOLE = W == Width::Whole;
     typedef Raw<BF, TINY> R;
     __shared__ __align__(16) T room[2][Across<T, WAVES>::kParts];
     Across<T, WAVES> across{room, 0};
@@ -177,7 +181,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
         skip[u] = TINY ? (at ? 8 : 0) : min(at - col[u], 8);
     }
     const int n = TINY ? a.H : 8;
-    auto mine = [&](int u, int i) { return i >= skip[u] && (!TINY || i < a.H); };
+    auto mine = [&](int u, int i) { return WHOLE || (i >= skip[u] && (!TINY || i < a.H)); };
+    auto behind = [&](int u) { return WHOLE && skip[u] == 8; };
     auto take = [&](const Rows &r, int u) {
         R v;
         v.load(r.data, r.f32, row * r.stride + col[u], n);
@@ -223,7 +228,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
 #pragma unroll
             for (int u = 0; u < V; ++u)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[u][i] -= mean;
+                for (int i = 0; i < 8; ++i) x[u][i] = behind(u) ? T(0) : x[u][i] - mean;
         }
         T ss = T(0);
 #pragma unroll
@@ -233,13 +238,22 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
         return inverse_root(fma(across.sum(ss), (T)a.inv_h, (T)eps));
     };
     const T offset = (T)a.weight_offset;
+    auto weigh = [&](int u, const R &w) {
+        if (a.weight_offset == 0.f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[u][i] *= (T)w.get(a.param_f32, i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[u][i] *= (T)w.get(a.param_f32, i) + offset;
+        }
+    };
     if (block) {
 #pragma unroll
         for (int u = 0; u < V; ++u) {
             apart();
             const R r = EARLY ? rb[EARLY ? u : 0] : take(a.block, u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = (T)r.get(a.block.f32, i);
+            for (int i = 0; i < 8; ++i) x[u][i] = behind(u) ? T(0) : (T)r.get(a.block.f32, i);
         }
         T by = (T)a.block_scale;
         if (a.post != ECHO_NORM_NONE) {
@@ -248,9 +262,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
 #pragma unroll
                 for (int u = 0; u < V; ++u) {
                     apart();
-                    const R w = EARLY ? rw[EARLY ? u : 0] : param(a.post_w, u);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[u][i] *= (T)w.get(a.param_f32, i) + offset;
+                    weigh(u, EARLY ? rw[EARLY ? u : 0] : param(a.post_w, u));
                 }
             }
             if (a.post_b) {
@@ -259,7 +271,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
                     apart();
                     const R w = param(a.post_b, u);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[u][i] = fma(x[u][i], inv, (T)w.get(a.param_f32, i));
+                    for (int i = 0; i < 8; ++i) x[u][i] = behind(u) ? T(0) : fma(x[u][i], inv, (T)w.get(a.param_f32, i));
                 }
             } else {
                 by *= inv;
@@ -287,7 +299,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
             const R r = EARLY ? rr[EARLY ? u : 0] : take(a.residual, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const T f = (T)r.get(a.residual.f32, i);
+                const T f = behind(u) ? T(0) : (T)r.get(a.residual.f32, i);
                 x[u][i] = block ? fma(f, by, x[u][i]) : f * by;
             }
         }
@@ -312,9 +324,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
 #pragma unroll
             for (int u = 0; u < V; ++u) {
                 apart();
-                const R w = EARLY ? rw2[EARLY ? u : 0] : param(a.pre_w, u);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[u][i] *= (T)w.get(a.param_f32, i) + offset;
+                weigh(u, EARLY ? rw2[EARLY ? u : 0] : param(a.pre_w, u));
             }
         }
         if (a.pre_b) {
@@ -323,7 +333,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
                 apart();
                 const R w = param(a.pre_b, u);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[u][i] = fma(x[u][i], inv, (T)w.get(a.param_f32, i));
+                for (int i = 0; i < 8; ++i) x[u][i] = behind(u) ? T(0) : fma(x[u][i], inv, (T)w.get(a.param_f32, i));
             }
             inv = T(1);
         }
@@ -339,23 +349,27 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
         }
     } else {
         // y is x inv; the largest of one is the largest of the other's
-        T top = T(0);
-        bool nan = false;
+        T top = T(0), odds = T(0);   // odds: 0, or NaN where an infinity or a NaN is
 #pragma unroll
         for (int u = 0; u < V; ++u)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 if (TINY && !mine(u, i)) continue;
                 top = fmax(top, fabs(x[u][i]));
-                nan |= x[u][i] != x[u][i];
+                odds = fma(x[u][i], T(0), odds);
             }
-        top = across.max(nan ? (T)INFINITY : top) * inv;
-        float s = (float)(top / T(127));
+        top = across.max(odds == T(0) ? top : (T)INFINITY) * inv;
+        // top / 127, its product with 1 / 127 corrected by the residual
+        constexpr double k127 = 1.0 / 127.0;
+        const T part = top * k127;
+        float s = (float)(top < (T)INFINITY ? fma(fma(-part, T(127), top), k127, part) : top);
         if (s == 0.f) s = 1.f;
         const bool odd = !(s < INFINITY);
         if (odd) s = __uint_as_float(0x7FC00000u);
         if (lane == 0) a.y_scale[row] = s;
-        const T by = T(1) / (T)s, both = by * inv;
+        // 1 / s: v_rcp_f64 is good to 2^-24 and better, a step of third order leaves 2^-70
+        const T r0 = __builtin_amdgcn_rcp((T)s), e0 = fma(-(T)s, r0, T(1));
+        const T by = fma(r0 * e0, e0 + T(1), r0), both = by * inv;
         // a quotient corrected by its residual is exact where it is a tie, as those of sums
         // that no norm has touched may be; scales that are hardly numbers leave some past 127
         const bool plain = a.pre != ECHO_NORM_NONE && s >= 0x1p-100f;
@@ -395,12 +409,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
     }
 }
 
-template <typename T, int WAVES, int V, bool BF, bool TINY = false>
+template <typename T, int WAVES, int V, bool BF, Width W>
 hipError_t launch(const Args &a, hipStream_t st) {
     constexpr int64_t kMost = 1 << 22;   // a launch has fewer than 2^32 threads
     const int64_t grid = WAVES == 1 ? ((int64_t)a.rows + 3) / 4 : a.rows;
     for (int64_t first = 0; first < grid; first += kMost) {
-        hipLaunchKernelGGL((join_kernel<T, WAVES, V, BF, TINY>), dim3((unsigned)std::min(kMost, grid - first)),
+        hipLaunchKernelGGL((join_kernel<T, WAVES, V, BF, W>), dim3((unsigned)std::min(kMost, grid - first)),
                            dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, st, a, (uint32_t)first);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -408,16 +422,25 @@ hipError_t launch(const Args &a, hipStream_t st) {
     return hipSuccess;
 }
 
-template <typename T, bool BF>
+template <typename T, bool BF, Width W>
 hipError_t launch_by_width(const Args &a, hipStream_t st) {
-    if (a.H < 8) return launch<T, 1, 1, false, true>(a, st);
-    if (a.H <= 512) return launch<T, 1, 1, BF>(a, st);
-    if (a.H <= 2048) return launch<T, 4, 1, BF>(a, st);
-    if (a.H <= 4096) return launch<T, 8, 1, BF>(a, st);
-    if (a.H <= 8192) return launch<T, 8, 2, BF>(a, st);
-    if (a.H <= 16384) return launch<T, 8, 4, BF>(a, st);
-    if constexpr (sizeof(T) == 4) return launch<T, 16, 4, BF>(a, st);
+    if (a.H <= 512) return launch<T, 1, 1, BF, W>(a, st);
+    if (a.H <= 2048) return launch<T, 4, 1, BF, W>(a, st);
+    if (a.H <= 4096) {
+        if constexpr (sizeof(T) == 8)
+            if (a.rows > kFewRows) return launch<T, 4, 2, BF, W>(a, st);
+        return launch<T, 8, 1, BF, W>(a, st);
+    }
+    if (a.H <= 8192) return launch<T, 8, 2, BF, W>(a, st);
+    if (a.H <= 16384) return launch<T, 8, 4, BF, W>(a, st);
+    if constexpr (sizeof(T) == 4) return launch<T, 16, 4, BF, W>(a, st);
     return hipErrorInvalidValue;   // codes: refused above
+}
+
+template <typename T, bool BF>
+hipError_t launch_join(const Args &a, hipStream_t st) {
+    if (a.H < 8) return launch<T, 1, 1, false, Width::Tiny>(a, st);
+    return a.H % 8 == 0 ? launch_by_width<T, BF, Width::Whole>(a, st) : launch_by_width<T, BF, Width::Odd>(a, st);
 }
 
 // rows of a tensor that a call names, checked; `codes`: int8 ones are allowed
@@ -515,8 +538,8 @@ int echo_norm_join(const echo_norm_t *norm, int32_t num_tokens, const echo_rows_
     bool bf = !a.param_f32;
     for (const Rows &r : {a.block, a.gate, a.residual, a.sum, a.y}) bf &= !r.f32;
     const hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = codes ? (bf ? launch_by_width<double, true>(a, st) : launch_by_width<double, false>(a, st))
-                               : (bf ? launch_by_width<float, true>(a, st) : launch_by_width<float, false>(a, st));
+    const hipError_t e = codes ? (bf ? launch_join<double, true>(a, st) : launch_join<double, false>(a, st))
+                               : (bf ? launch_join<float, true>(a, st) : launch_join<float, false>(a, st));
     return e == hipSuccess ? ECHO_OK : fail(ECHO_E_HIP, "echo_norm_join: %s", hipGetErrorString(e));
 }
 
