@@ -67,6 +67,10 @@ struct Raw {
             }
         }
     }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < (BF ? 1 : 2); ++i) a[i] = (u32x4){0u, 0u, 0u, 0u};
+    }
     __device__ __forceinline__ float get(int f32, int i) const {
         const uint32_t half = i & 1 ? a[0][i / 2] & 0xFFFF0000u : a[0][i / 2] << 16;
         if constexpr (BF) return __uint_as_float(half);
@@ -98,44 +102,64 @@ __device__ __forceinline__ void store8(uint8_t *p, int f32, int64_t at, int n, c
     }
 }
 
-// Sums and maxima over a row's WAVES waves, a barrier each: the lanes of sixteen meet
-// by DPP, the rest in LDS, in places that take turns.
+// Sums and maxima over a row's WAVES waves: the lanes of sixteen meet by DPP, those of
+// a wave by swapping rows, the waves in LDS, a barrier each, in places that take turns.
 template <int CTRL>
-__device__ __forceinline__ float turned(float v) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
+__device__ __forceinline__ uint32_t turned(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
 }
-template <int CTRL>
-__device__ __forceinline__ double turned(double v) {
-    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xF, 0xF, false);
-    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xF, 0xF, false);
-    return __hiloint2double(hi, lo);
+template <int LANES>
+__device__ __forceinline__ void swapped(uint32_t v, uint32_t &x, uint32_t &y) {   // rows of v, and their neighbours'
+    if constexpr (LANES == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        x = r[0], y = r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        x = r[0], y = r[1];
+    }
+}
+template <int CTRL, typename F>
+__device__ __forceinline__ float meet(float v, F join) {
+    return join(v, __uint_as_float(turned<CTRL>(__float_as_uint(v))));
+}
+template <int CTRL, typename F>
+__device__ __forceinline__ double meet(double v, F join) {
+    return join(v, __hiloint2double((int)turned<CTRL>((uint32_t)__double2hiint(v)), (int)turned<CTRL>((uint32_t)__double2loint(v))));
+}
+template <int LANES, typename F>
+__device__ __forceinline__ float meet_rows(float v, F join) {
+    uint32_t x, y;
+    swapped<LANES>(__float_as_uint(v), x, y);
+    return join(__uint_as_float(x), __uint_as_float(y));
+}
+template <int LANES, typename F>
+__device__ __forceinline__ double meet_rows(double v, F join) {
+    uint32_t xl, yl, xh, yh;
+    swapped<LANES>((uint32_t)__double2loint(v), xl, yl);
+    swapped<LANES>((uint32_t)__double2hiint(v), xh, yh);
+    return join(__hiloint2double((int)xh, (int)xl), __hiloint2double((int)yh, (int)yl));
 }
 
 template <typename T, int WAVES>
 struct Across {
-    static constexpr bool kWide = WAVES > 4;   // waves meet first
-    static constexpr int kParts = WAVES == 1 ? 1 : kWide ? WAVES : 4 * WAVES;
-    T (*room)[kParts];
+    T (*room)[WAVES];
     int turn;
     template <typename F>
     __device__ __forceinline__ T all(T v, F join) {
-        v = join(v, turned<0x128>(v));   // row_ror:8, 4, 2, 1
-        v = join(v, turned<0x124>(v));
-        v = join(v, turned<0x122>(v));
-        v = join(v, turned<0x121>(v));
-        if constexpr (WAVES == 1 || kWide) {
-            v = join(v, __shfl_xor(v, 16));
-            v = join(v, __shfl_xor(v, 32));
-        }
+        v = meet<0x128>(v, join);   // row_ror:8, 4, 2, 1
+        v = meet<0x124>(v, join);
+        v = meet<0x122>(v, join);
+        v = meet<0x121>(v, join);
+        v = meet_rows<16>(v, join);
+        v = meet_rows<32>(v, join);
         if constexpr (WAVES > 1) {
             T *part = room[turn];
             turn ^= 1;
-            constexpr int LANES = kWide ? 64 : 16;
-            if (threadIdx.x % LANES == 0) part[threadIdx.x / LANES] = v;
+            if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
             __syncthreads();
             v = part[0];
 #pragma unroll
-            for (int w = 1; w < kParts; ++w) v = join(v, part[w]);
+            for (int w = 1; w < WAVES; ++w) v = join(v, part[w]);
         }
         return v;
     }
@@ -159,12 +183,17 @@ __device__ __forceinline__ double inverse_root(double x) {
 // The last eight of a row begin at H - 8, whatever H is a multiple of: what a lane
 // before them has too counts for that one alone (`skip`), and comes out the same, to be
 // written twice.  In rows of whole eights lanes behind the end hold zeros.  Where V <= 2 every input is asked for before the first sum.
-template <typename T, int WAVES, int V, bool BF, Width W>
+template <typename T, int WAVES, int V, bool BF, Width W, bool LEAN>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Args a, uint32_t first) {
+    if (LEAN) {
+        a.post = a.pre = ECHO_NORM_RMS;
+        a.post_b = a.pre_b = nullptr;
+        a.weight_offset = 0.f;
+    }
     constexpr int LANES = 64 * WAVES;
     constexpr bool EARLY = V <= 2, TINY = W == Width::Tiny, WHOLE = W == Width::Whole;
     typedef Raw<BF, TINY> R;
-    __shared__ __align__(16) T room[2][Across<T, WAVES>::kParts];
+    __shared__ __align__(16) T room[2][WAVES];
     Across<T, WAVES> across{room, 0};
     const int lane = threadIdx.x % LANES;
     int64_t row = WAVES == 1 ? 4 * ((int64_t)first + blockIdx.x) + threadIdx.x / 64 : (int64_t)first + blockIdx.x;
@@ -193,7 +222,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
         v.load(p, a.param_f32, col[u], n);
         return v;
     };
-    const bool block = a.block.data, gate = block && a.gate.data, residual = a.residual.data, y = a.y.data;
+    const bool block = LEAN || a.block.data, gate = block && a.gate.data, residual = LEAN || a.residual.data;
+    const bool y = LEAN || a.y.data, post_w = LEAN || a.post_w, pre_w = LEAN || a.pre_w;
     R rb[EARLY ? V : 1], rg[EARLY ? V : 1], rr[EARLY ? V : 1], rw[EARLY ? V : 1], rw2[EARLY ? V : 1];
     if constexpr (EARLY) {
 #pragma unroll
@@ -203,8 +233,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
         for (int u = 0; u < V; ++u) {
             if (residual) rr[u] = take(a.residual, u);
             if (gate) rg[u] = take(a.gate, u);
-            if (a.post_w) rw[u] = param(a.post_w, u);
-            if (a.pre_w) rw2[u] = param(a.pre_w, u);
+            if (post_w) rw[u] = param(a.post_w, u);
+            if (pre_w) rw2[u] = param(a.pre_w, u);
         }
     }
     auto apart = [] {   // loads of the next unit wait for this one's registers
@@ -251,14 +281,15 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
 #pragma unroll
         for (int u = 0; u < V; ++u) {
             apart();
-            const R r = EARLY ? rb[EARLY ? u : 0] : take(a.block, u);
+            R r = EARLY ? rb[EARLY ? u : 0] : take(a.block, u);
+            if (behind(u)) r.clear();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = behind(u) ? T(0) : (T)r.get(a.block.f32, i);
+            for (int i = 0; i < 8; ++i) x[u][i] = (T)r.get(a.block.f32, i);
         }
         T by = (T)a.block_scale;
         if (a.post != ECHO_NORM_NONE) {
             const T inv = inverse(a.post, a.post_eps);
-            if (a.post_w) {
+            if (post_w) {
 #pragma unroll
                 for (int u = 0; u < V; ++u) {
                     apart();
@@ -296,10 +327,11 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
 #pragma unroll
         for (int u = 0; u < V; ++u) {
             apart();
-            const R r = EARLY ? rr[EARLY ? u : 0] : take(a.residual, u);
+            R r = EARLY ? rr[EARLY ? u : 0] : take(a.residual, u);
+            if (behind(u)) r.clear();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const T f = behind(u) ? T(0) : (T)r.get(a.residual.f32, i);
+                const T f = (T)r.get(a.residual.f32, i);
                 x[u][i] = block ? fma(f, by, x[u][i]) : f * by;
             }
         }
@@ -320,7 +352,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
     T inv = T(1);
     if (a.pre != ECHO_NORM_NONE) {
         inv = inverse(a.pre, a.pre_eps);
-        if (a.pre_w) {
+        if (pre_w) {
 #pragma unroll
             for (int u = 0; u < V; ++u) {
                 apart();
@@ -409,12 +441,20 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Arg
     }
 }
 
-template <typename T, int WAVES, int V, bool BF, Width W>
+// both norms the usual ones: RMS with weights alone
+bool lean(const Args &a) {
+    return a.post == ECHO_NORM_RMS && a.pre == ECHO_NORM_RMS && a.post_w && a.pre_w && !a.post_b && !a.pre_b &&
+           a.weight_offset == 0.f && a.block.data && a.residual.data && a.y.data;
+}
+
+template <typename T, int WAVES, int V, bool BF, Width W, bool LEAN = false>
 hipError_t launch(const Args &a, hipStream_t st) {
+    if constexpr (!LEAN && BF && W == Width::Whole && V <= 2)
+        if (lean(a)) return launch<T, WAVES, V, BF, W, true>(a, st);
     constexpr int64_t kMost = 1 << 22;   // a launch has fewer than 2^32 threads
     const int64_t grid = WAVES == 1 ? ((int64_t)a.rows + 3) / 4 : a.rows;
     for (int64_t first = 0; first < grid; first += kMost) {
-        hipLaunchKernelGGL((join_kernel<T, WAVES, V, BF, W>), dim3((unsigned)std::min(kMost, grid - first)),
+        hipLaunchKernelGGL((join_kernel<T, WAVES, V, BF, W, LEAN>), dim3((unsigned)std::min(kMost, grid - first)),
                            dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, st, a, (uint32_t)first);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

@@ -107,6 +107,17 @@ def test_forms(T, H, kw, gate, block, residual):
         _case(g, T, H, kw, types, pad=5 if T % 2 else 0, gate=gate, block=block, residual=residual)
 
 
+@pytest.mark.parametrize("ty", ["bf16", "i8"])
+@pytest.mark.parametrize("H", [8, 16, 512, 1000, 2048, 2056, 4096, 4104, 8192])
+def test_two_rms_norms_in_bf16(H, ty):
+    """The usual pair of norms, few rows and many."""
+    g = np.random.default_rng(H + 1)
+    say(f"[case] two RMS norms of {H} to {ty}")
+    for T, gate, pad in [(3, None, 0), (4, "channel", 8), (600, "token", 0)]:
+        _case(g, T, H, dict(post="rms", pre="rms", post_weight=True, pre_weight=True, block_scale=0.5),
+              ("bf16", "bf16", "bf16" if T != 3 else None, ty, "bf16"), gate=gate, pad=pad)
+
+
 @pytest.mark.parametrize("H", [48, 4096])
 def test_in_place(H):
     import torch
