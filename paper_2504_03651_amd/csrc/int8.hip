@@ -151,20 +151,21 @@ constexpr int rows_depth(int NT, int XR) { return std::min(6, 160 * 1024 / (kStr
 constexpr int rows_tokens(int T) { return T <= 8 ? 8 : T <= 16 ? 16 : 32; }
 
 // How a product is cut: the kernel's form, and how many ranges of K there are.
-enum Form { kRows16, kRows32, k64x32, k64x64, k128x64, k128x128, k256x128, k256x256 };
+enum Form { kRows16, kRows32, k64x32, k64x64, k128x64, k128x128, k256x128, k256x192 };
 struct Cut {
     Form form;
     int ranges;
 };
 
-// Tiles n x t: what a step of 128 of K takes with one workgroup on a CU, and with two
-// where LDS holds two
+// Tiles n x t, in microseconds: what a step of 128 of K takes with one workgroup on a CU,
+// and with two where LDS holds two; the launch; going on to another tile
 constexpr struct {
     Form form;
     int n, t;
-    double one, two;
-} kTileForms[] = {{k64x32, 64, 32, .37, .52},   {k64x64, 64, 64, .45, .75}, {k128x64, 128, 64, .68, 1.0},
-                  {k128x128, 128, 128, .88, 0}, {k256x128, 256, 128, 1.32, 0}, {k256x256, 256, 256, 2.0, 0}};
+    double one, two, launch, on;
+} kTileForms[] = {{k64x32, 64, 32, .25, .43, 3.2, 2.},   {k64x64, 64, 64, .40, .48, 3.5, 2.},
+                  {k128x64, 128, 64, .54, .75, 3.45, 2.}, {k128x128, 128, 128, .59, 0, 3.5, 2.},
+                  {k256x128, 256, 128, .76, 0, 3.45, 1.9}, {k256x192, 256, 192, 1.13, 0, 3.9, 3.1}};
 constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16};
 
 // Products of more tiles, or whose parts would take more, are not cut into ranges of K,
@@ -191,7 +192,16 @@ size_t most_parts_bytes(int T, int N, int K) {
     return std::min<size_t>((size_t)rows * pitch_of(N) * 4, kPartBytes);
 }
 
-// The cut of least estimated time, in microseconds.
+// The cut of least estimated time, in microseconds fitted to bf16 results of 430 sizes (T 1
+// to 4,640, N 64 to 28,672, K 128 to 14,336, weights from memory): 0.7% (geometric mean)
+// above the best cut of each, 25% at most (20 x 17342 x 8256, where four ranges of K would
+// be best); over 130 sizes with fp32 results 1.1% and 21%.
+//   Weights and tokens come at 5.0 TB/s at most.
+//   kRows: 16 or 32 weight rows a workgroup, every wave on its own; one workgroup a
+//   CU, which takes in 70 KB a microsecond, tokens among them (8 x 6144 x 4096: 7.2 by 32
+//   rows; 64 x 32 tiles take over where a CU has more than one: 8 x 10911 x 3056 14.4
+//   and 11.7).
+//   Ranges of K cost a second launch and their sums' way to memory and back.
 Cut cut_of(int T, int N, int K) {
     const int KB = cdiv(K, kStep);
     const double bytes = (double)N * K + (double)T * K;
@@ -201,21 +211,21 @@ Cut cut_of(int T, int N, int K) {
         const int x = rows_tokens(T);
         const int64_t turns = ((int64_t)cdiv(N, 16 * nt) * cdiv(T, x > 16 ? 32 : 16) + 255) / 256;
         if (turns >= 1 << 14) continue;   // a launch has fewer than 2^32 threads
-        const double us = std::max(bytes / 5.2e6, (double)turns * (16 * nt + x) * K / 50e3) + 0.6 +
+        const double us = std::max(bytes / 5.0e6, (double)turns * (16 * nt + x) * K / 70e3) + 2.6 +
                           1.5 * (double)(turns - 1);
         if (us < least) least = us, best = Cut{nt == 1 ? kRows16 : kRows32, 1};
     }
     for (const auto &f : kTileForms) {
-        if (f.t > 32 && T <= f.t / 2) continue;
+        if (f.t > 32 && T <= f.t / 3) continue;
         for (int s : kRanges) {
             const int64_t all = (int64_t)cdiv(N, f.n) * cdiv(T, f.t) * s;
             if (s > 1 && (2 * s > KB || all > kRangeTiles || parts_bytes(s, T, N) > kPartBytes)) break;
             const int64_t each = (all + 255) / 256;   // of a CU
             const double turns = f.two > 0 ? (double)(each / 2) * f.two + (double)(each % 2) * f.one
                                            : (double)each * f.one;
-            const double starts = (double)(f.two > 0 ? (each + 1) / 2 : each) - 1;
-            double us = std::max(cdiv(KB, s) * turns + 2.5 * starts, bytes / 5.2e6);
-            if (s > 1) us += 3.4 + 0.25 * s + 8.0 * s * T * N / 5e6;
+            const double on = f.on * (double)((f.two > 0 ? (each + 1) / 2 : each) - 1);
+            double us = std::max(cdiv(KB, s) * turns + on, bytes / 5.0e6) + f.launch;
+            if (s > 1) us += 2.5 + 0.2 * s + 8.0 * s * T * N / 4.6e6;
             if (us < least) least = us, best = Cut{f.form, s};
         }
     }
@@ -233,11 +243,11 @@ hipError_t launch_rows(const Product &p, hipStream_t st) {
     }
 }
 
-template <bool F32, int BN, int BT, int WN, int WT, int S>
+template <bool F32, int BN, int BT, int WN, int WT, int STEP, int S>
 hipError_t launch_tiles(const Product &p, int ranges, hipStream_t st) {
     if constexpr (BT <= 64)
-        if (p.T <= BT) return launch_tiled<F32, true, BN, BT, WN, WT, S>(p, ranges, st);
-    return launch_tiled<F32, false, BN, BT, WN, WT, S>(p, ranges, st);
+        if (p.T <= BT) return launch_tiled<F32, true, BN, BT, WN, WT, STEP, S>(p, ranges, st);
+    return launch_tiled<F32, false, BN, BT, WN, WT, STEP, S>(p, ranges, st);
 }
 
 template <bool F32>
@@ -246,12 +256,13 @@ hipError_t launch_gemm(const Product &p, Cut c, hipStream_t st) {
     switch (c.form) {
         case kRows16: return launch_rows<F32, 1>(p, st);
         case kRows32: return launch_rows<F32, 2>(p, st);
-        case k64x32: e = launch_tiles<F32, 64, 32, 4, 1, 5>(p, c.ranges, st); break;
-        case k64x64: e = launch_tiles<F32, 64, 64, 4, 1, 4>(p, c.ranges, st); break;
-        case k128x64: e = launch_tiles<F32, 128, 64, 4, 1, 3>(p, c.ranges, st); break;
-        case k128x128: e = launch_tiles<F32, 128, 128, 4, 2, 4>(p, c.ranges, st); break;
-        case k256x128: e = launch_tiles<F32, 256, 128, 4, 2, 3>(p, c.ranges, st); break;
-        case k256x256: e = launch_tiles<F32, 256, 256, 2, 4, 2>(p, c.ranges, st); break;
+        case k64x32: e = launch_tiles<F32, 64, 32, 4, 1, 128, 6>(p, c.ranges, st); break;
+        case k64x64: e = launch_tiles<F32, 64, 64, 4, 1, 128, 4>(p, c.ranges, st); break;
+        case k128x64: e = launch_tiles<F32, 128, 64, 4, 1, 128, 3>(p, c.ranges, st); break;
+        case k128x128: e = launch_tiles<F32, 128, 128, 4, 2, 128, 4>(p, c.ranges, st); break;
+        case k256x128: e = launch_tiles<F32, 256, 128, 4, 2, 128, 3>(p, c.ranges, st); break;
+        // (fp32 results of such tiles would spill registers)
+        case k256x192: e = launch_tiles<F32, 256, F32 ? 128 : 192, 4, 2, 128, F32 ? 3 : 2>(p, c.ranges, st); break;
     }
     if (e != hipSuccess || c.ranges == 1 || (e = hipGetLastError()) != hipSuccess) return e;
     const int64_t n = (int64_t)p.T * (p.part_pitch / 4);

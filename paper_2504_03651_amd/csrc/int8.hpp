@@ -62,8 +62,8 @@ __device__ __forceinline__ float scaled(int sum, Scale x, Scale w) {
 }
 
 // E columns from n of row t, whose scaled sums with bias are v: the residual is added,
-// and y written
-template <bool F32, int E>
+// and y written; PAST: past the caches
+template <bool F32, int E, bool PAST = false>
 __device__ __forceinline__ void put(const Product &p, int64_t t, int n, float (&v)[E]) {
     static_assert(E == 4 || E == 8);
     const int64_t at = t * p.y_stride + n;
@@ -73,7 +73,8 @@ __device__ __forceinline__ void put(const Product &p, int64_t t, int n, float (&
             for (int e = 0; e < E; e += 4) {
                 f32x4 o = {v[e], v[e + 1], v[e + 2], v[e + 3]};
                 if (p.residual) o += *(const any_f32x4 *)((const float *)p.residual + at + e);
-                *(any_f32x4 *)((float *)p.y + at + e) = o;
+                if (PAST) __builtin_nontemporal_store(o, (any_f32x4 *)((float *)p.y + at + e));
+                else *(any_f32x4 *)((float *)p.y + at + e) = o;
             }
         } else {
             uint32_t o[E / 2];
@@ -90,7 +91,10 @@ __device__ __forceinline__ void put(const Product &p, int64_t t, int n, float (&
             }
 #pragma unroll
             for (int e = 0; e < E / 2; ++e) o[e] = f2bf2(v[2 * e], v[2 * e + 1]);
-            if constexpr (E == 8) *(any_u32x4 *)((uint16_t *)p.y + at) = (u32x4){o[0], o[1], o[2], o[3]};
+            if constexpr (E == 8 && PAST)
+                __builtin_nontemporal_store((u32x4){o[0], o[1], o[2], o[3]}, (any_u32x4 *)((uint16_t *)p.y + at));
+            else if constexpr (E == 8)
+                *(any_u32x4 *)((uint16_t *)p.y + at) = (u32x4){o[0], o[1], o[2], o[3]};
             else *(any_u32x2 *)((uint16_t *)p.y + at) = (u32x2){o[0], o[1]};
         }
         return;
