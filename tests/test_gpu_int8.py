@@ -150,6 +150,11 @@ SIZES = [(1, 1, 16), (1, 16, 16), (2, 17, 48), (3, 5, 144), (8, 1024, 4096), (8,
          (17, 260, 128), (31, 67, 2064), (32, 6000, 256), (33, 70, 2064), (48, 4096, 512), (64, 129, 8208), (65, 130, 1040),
          (67, 1000, 2064), (100, 515, 272), (128, 128, 128), (129, 257, 400), (137, 4096, 1040), (200, 300, 4112),
          (256, 256, 256), (257, 511, 384), (513, 260, 144), (1000, 3001, 272), (1031, 6150, 528)]
+# each tile in one range of K and in several, the last tiles of tokens and columns cut off
+SIZES += [(34, 4185, 16), (17, 1, 11296), (34, 1, 11104), (160, 6001, 4112), (35, 17615, 16), (45, 20001, 2064),
+          (34, 4107, 5344), (132, 16617, 16), (132, 16617, 400), (33, 4131, 5680), (66, 16935, 16), (70, 16935, 656),
+          (70, 5579, 3392), (203, 16699, 16), (203, 16699, 528), (133, 2713, 10192), (398, 16971, 16), (398, 16971, 656),
+          (770, 19001, 272), (130, 10939, 8160)]
 
 
 @pytest.mark.parametrize("f32", [True, False])
