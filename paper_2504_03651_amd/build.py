@@ -1,4 +1,5 @@
-"""Builds libecho.so in-tree with hipcc for gfx950 (no JIT, no cache).
+"""Builds libecho.so in-tree with hipcc for gfx950, and the bindings' compiled part
+_binding.so with g++ (no JIT, no cache).
 
 ``build_sanitized()`` builds a copy whose host code (the planner, the block
 manager and the validation in the C ABI) carries AddressSanitizer and
@@ -24,6 +25,31 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
 
+BINDING = os.path.join(PKG, "_binding.so")
+
+
+def build_binding(verbose: bool = False) -> str:
+    """The compiled part of the Python bindings (host code only), against PyTorch's headers."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    tmp = BINDING + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(root, "include"),
+           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "binding.cpp"), "-o", tmp,
+           "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        sys.stderr.write(r.stdout + r.stderr)
+        raise RuntimeError("g++ failed on binding.cpp")
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 def build(verbose: bool = False) -> str:
     bdir = os.path.join(ROOT, "_build")
     os.makedirs(bdir, exist_ok=True)
@@ -46,6 +72,7 @@ def build(verbose: bool = False) -> str:
         sys.stderr.write(r.stdout + r.stderr)
         raise RuntimeError("link of libecho.so failed")
     os.replace(tmp, OUT)
+    build_binding(verbose)
     return OUT
 
 

@@ -8,20 +8,18 @@ from __future__ import annotations
 
 import ctypes
 
-from . import echo, fp8
-from .fp8 import BF16, F32, address, refuse, rows, scratch, sizes, stream_of
+from . import echo, native
+from .fp8 import sizes
 
 SYMBOLS = ["echo_int8_quantize", "echo_int8_gemm", "echo_int8_gemm_workspace_bytes"]
 
 _bound = False
-_codes = None
 
 
 def _lib():
-    global _bound, _codes
+    global _bound
     L = echo.lib()
     if not _bound:
-        import torch
         vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         L.echo_int8_quantize.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp]
         L.echo_int8_quantize.restype = ctypes.c_int
@@ -29,7 +27,6 @@ def _lib():
         L.echo_int8_gemm_workspace_bytes.restype = sz
         L.echo_int8_gemm.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, i32, i64, vp, sz, vp]
         L.echo_int8_gemm.restype = ctypes.c_int
-        _codes = (torch.int8,)
         _bound = True
     return L
 
@@ -37,21 +34,7 @@ def _lib():
 def quantize(x, codes, scales, stream=None) -> None:
     """Codes and scales of the rows of ``x`` [rows][cols] (any distance apart), bf16 or
     fp32."""
-    where, k, L = "echo_int8_quantize", fp8.types(), _lib()
-    dev = k.device()
-    shape = x.shape
-    if len(shape) != 2:
-        refuse(where, f"x has {x.dim()} axes")
-    n, cols = shape
-    if (n | cols) >> 31:
-        sizes(where, n, cols)
-    xp, stride = rows(where, "x", x, shape, k.real, dev)
-    cp = address(where, "codes", codes, shape, _codes, dev)
-    sp = address(where, "scales", scales, (n,), k.f32, dev)
-    rc = L.echo_int8_quantize(xp, F32 if x.dtype is k.f32[0] else BF16, stride, n, cols, cp, sp,
-                              stream_of(stream, dev))
-    if rc:
-        echo._check(rc, where)
+    native.binding().quantize(x, codes, scales, stream)
 
 
 def gemm_workspace_bytes(num_tokens: int, out_features: int, in_features: int) -> int:
@@ -69,26 +52,4 @@ def gemm(x, x_scale, w, w_scale, out, bias=None, residual=None, workspace=None, 
     transpose of w [N][K], plus ``bias`` (fp32 [N]), plus ``residual`` (of out's type and
     strides; may be out itself).  ``workspace``: gemm_workspace_bytes() bytes, None
     where that is 0."""
-    where, k, L = "echo_int8_gemm", fp8.types(), _lib()
-    dev = k.device()
-    if x.dim() != 2 or w.dim() != 2:
-        refuse(where, f"x has {x.dim()} axes, w {w.dim()}")
-    (T, K), N = x.shape, w.shape[0]
-    if (T | K | N) >> 31:
-        sizes(where, T, K, N)
-    xp = address(where, "x", x, (T, K), _codes, dev)
-    xsp = address(where, "x_scale", x_scale, (T,), k.f32, dev)
-    wp = address(where, "w", w, (N, K), _codes, dev)
-    wsp = address(where, "w_scale", w_scale, (N,), k.f32, dev)
-    yp, stride = rows(where, "out", out, (T, N), k.real, dev)
-    bp = None if bias is None else address(where, "bias", bias, (N,), k.f32, dev)
-    rp = None
-    if residual is not None:
-        rp, rs = rows(where, "residual", residual, (T, N), k.real, dev)
-        if residual.dtype is not out.dtype or rs != stride:
-            refuse(where, "residual has not the type and strides of out")
-    sp, sb = scratch(where, workspace, dev)
-    rc = L.echo_int8_gemm(xp, xsp, wp, wsp, T, N, K, bp, rp, yp, F32 if out.dtype is k.f32[0] else BF16,
-                          stride, sp, sb, stream_of(stream, dev))
-    if rc:
-        echo._check(rc, where)
+    native.binding().gemm(x, x_scale, w, w_scale, out, bias, residual, workspace, stream)

@@ -4,8 +4,8 @@ from __future__ import annotations
 
 import ctypes
 
-from . import echo, fp8
-from .fp8 import BF16, F32, address, refuse, sizes, stream_of
+from . import echo, native
+from .fp8 import refuse, sizes
 
 SYMBOLS = ["echo_rope_frequencies", "echo_rope_rotate"]
 
@@ -62,9 +62,9 @@ class Rope:
         self.head_dim, self.rotary_dim = head_dim, rotary_dim
         self.c = CRope(head_dim, rotary_dim, LAYOUTS[layout], SCALINGS[scaling], theta, factor, low, high,
                        original_length)
-        self.ref = ctypes.byref(self.c)
+        self.at = ctypes.addressof(self.c)
         f, m = (ctypes.c_double * max(1, rotary_dim // 2))(), ctypes.c_double()
-        echo._check(_lib().echo_rope_frequencies(self.ref, f, ctypes.byref(m)), "echo_rope_frequencies")
+        echo._check(_lib().echo_rope_frequencies(ctypes.byref(self.c), f, ctypes.byref(m)), "echo_rope_frequencies")
         if frequencies is None:
             frequencies = list(f)
         self.frequencies = torch.as_tensor(frequencies, dtype=torch.float64, device=device).contiguous()
@@ -73,60 +73,10 @@ class Rope:
         self.magnitude = float(m.value if magnitude is None else magnitude)
 
 
-def _heads(where, name, x, T, D, dtypes, dev):
-    """(address, heads, elements from token to token and from head to head)"""
-    if x.dim() != 3 or x.shape[0] != T or x.shape[2] != D:
-        refuse(where, f"{name} has shape {tuple(x.shape)}, not ({T}, heads, {D})")
-    if x.dtype not in dtypes:
-        refuse(where, f"{name} has dtype {x.dtype}")
-    if x.get_device() != dev:
-        fp8._place(where, name, x, dev)
-    t, h, one = x.stride()
-    if one != 1:
-        refuse(where, f"the columns of {name} are not adjacent")
-    n = x.shape[1]
-    if n >> 31:
-        sizes(where, n)
-    # an axis of one has any stride
-    return x.data_ptr(), n, t if T > 1 else n * D, h if n > 1 else D
-
-
 def rotate(rope: Rope, positions, q, k=None, q_out=None, k_out=None, inverse: bool = False,
            stream=None) -> None:
     """Turns the heads of q [T][heads][D] and of k (bf16 or fp32, both alike, tokens and
     heads any distance apart) by ``positions`` (int32 [T]), into q_out and k_out or in
     place."""
-    where, ty = "echo_rope_rotate", fp8.types()
-    dev = ty.device()
-    if q.dim() != 3:
-        refuse(where, f"q has {q.dim()} axes")
-    T, D = q.shape[0], rope.head_dim
-    if T >> 31:
-        sizes(where, T)
-    if q.dtype not in ty.real:
-        refuse(where, f"q has dtype {q.dtype}")
-    dtypes = (q.dtype,)
-    if k is None and k_out is not None:
-        refuse(where, "k_out without k")
-    tensors = (CHeads * 2)()
-    n = 0
-    for name, x, out in (("q", q, q_out), ("k", k, k_out)):
-        if x is None:
-            continue
-        xp, heads, xt, xh = _heads(where, name, x, T, D, dtypes, dev)
-        op, ot, oh = xp, xt, xh
-        if out is not None:
-            op, out_heads, ot, oh = _heads(where, name + "_out", out, T, D, dtypes, dev)
-            if out_heads != heads:
-                refuse(where, f"{name}_out has {out_heads} heads, {name} {heads}")
-        tensors[n] = CHeads(xp, op, heads, xt, xh, ot, oh)
-        n += 1
-    pp = address(where, "positions", positions, (T,), ty.i32, dev)
-    f = rope.frequencies
-    if f.get_device() != dev:
-        fp8._place(where, "rope.frequencies", f, dev)
-    rc = _lib().echo_rope_rotate(rope.ref, f.data_ptr(), rope.magnitude, pp, T,
-                                 F32 if q.dtype is ty.f32[0] else BF16, tensors, n, int(inverse),
-                                 stream_of(stream, dev))
-    if rc:
-        echo._check(rc, where)
+    native.binding().rotate(rope.at, rope.frequencies, rope.magnitude, positions, q, k, q_out, k_out, inverse,
+                            stream)
