@@ -136,13 +136,23 @@ __global__ __launch_bounds__(256) void add_parts_kernel(Product p, int ranges) {
     if (i >= (int64_t)p.T * q) return;
     const int64_t t = i / q;
     const int n = 4 * (int)(i - t * q);
-    i32x4 s = *(const i32x4 *)(p.part + t * p.part_pitch + n);
-    for (int r = 1; r < ranges; ++r) s += *(const i32x4 *)(p.part + (r * (int64_t)p.T + t) * p.part_pitch + n);
     Columns<4> cols;
     cols.load(p, n);
+    const Scale xs = split(p.xs[t]);
+    const int32_t *from = p.part + t * p.part_pitch + n;
+    i32x4 s = {0, 0, 0, 0};
+    for (int r = 0; r < ranges; r += 4) {   // four at a time are under way
+        i32x4 more[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            more[k] = *(const i32x4 *)(from + min(r + k, ranges - 1) * (int64_t)p.T * p.part_pitch);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (r + k < ranges) s += more[k];
+    }
     const int sum[4] = {s[0], s[1], s[2], s[3]};
     float v[4];
-    cols.apply(p, sum, split(p.xs[t]), v);
+    cols.apply(p, sum, xs, v);
     put<F32, 4>(p, t, n, v);
 }
 
@@ -151,7 +161,7 @@ constexpr int rows_depth(int NT, int XR) { return std::min(6, 160 * 1024 / (kStr
 constexpr int rows_tokens(int T) { return T <= 8 ? 8 : T <= 16 ? 16 : 32; }
 
 // How a product is cut: the kernel's form, and how many ranges of K there are.
-enum Form { kRows16, kRows32, k64x32, k64x64, k128x64, k128x128, k256x128, k256x192 };
+enum Form { kRows16, kRows32, k64x32, k64x64, k128x64, k128x96, k128x128, k128x160, k256x128, k256x192 };
 struct Cut {
     Form form;
     int ranges;
@@ -163,9 +173,10 @@ constexpr struct {
     Form form;
     int n, t;
     double one, two, launch, on;
-} kTileForms[] = {{k64x32, 64, 32, .25, .43, 3.2, 2.},   {k64x64, 64, 64, .40, .48, 3.5, 2.},
-                  {k128x64, 128, 64, .54, .75, 3.45, 2.}, {k128x128, 128, 128, .59, 0, 3.5, 2.},
-                  {k256x128, 256, 128, .76, 0, 3.45, 1.9}, {k256x192, 256, 192, 1.13, 0, 3.9, 3.1}};
+} kTileForms[] = {{k64x32, 64, 32, .25, .41, 3.1, 2.},   {k64x64, 64, 64, .36, .42, 3.5, 2.},
+                  {k128x64, 128, 64, .54, .75, 3.3, 2.}, {k128x96, 128, 96, .57, 0, 3.3, 2.},
+                  {k128x128, 128, 128, .59, 0, 3.5, 2.},   {k128x160, 128, 160, .67, 0, 3.5, 2.},
+                  {k256x128, 256, 128, .77, 0, 3.5, 2.}, {k256x192, 256, 192, 1.16, 0, 4., 3.1}};
 constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16};
 
 // Products of more tiles, or whose parts would take more, are not cut into ranges of K,
@@ -194,15 +205,15 @@ size_t most_parts_bytes(int T, int N, int K) {
 
 // The cut of least estimated time, in microseconds fitted to bf16 results of 430 sizes (T 1
 // to 4,640, N 64 to 28,672, K 128 to 14,336, weights from memory): 0.7% (geometric mean)
-// above the best cut of each, 25% at most (20 x 17342 x 8256, where four ranges of K would
-// be best); over 130 sizes with fp32 results 1.1% and 21%.
+// above the best cut of each, 23% at most (20 x 17342 x 8256, where four ranges of K would
+// be best); over 130 sizes with fp32 results 0.7% and 21%.
 //   Weights and tokens come at 5.0 TB/s at most.
 //   kRows: 16 or 32 weight rows a workgroup, every wave on its own; one workgroup a
 //   CU, which takes in 70 KB a microsecond, tokens among them (8 x 6144 x 4096: 7.2 by 32
 //   rows; 64 x 32 tiles take over where a CU has more than one: 8 x 10911 x 3056 14.4
 //   and 11.7).
 //   Ranges of K cost a second launch and their sums' way to memory and back.
-Cut cut_of(int T, int N, int K) {
+Cut cut_of(int T, int N, int K, bool f32) {
     const int KB = cdiv(K, kStep);
     const double bytes = (double)N * K + (double)T * K;
     Cut best{kRows16, 1};
@@ -216,16 +227,16 @@ Cut cut_of(int T, int N, int K) {
         if (us < least) least = us, best = Cut{nt == 1 ? kRows16 : kRows32, 1};
     }
     for (const auto &f : kTileForms) {
-        if (f.t > 32 && T <= f.t / 3) continue;
+        if ((f.t > 32 && T <= f.t / 3) || (f32 && f.form == k256x192)) continue;
         for (int s : kRanges) {
             const int64_t all = (int64_t)cdiv(N, f.n) * cdiv(T, f.t) * s;
-            if (s > 1 && (2 * s > KB || all > kRangeTiles || parts_bytes(s, T, N) > kPartBytes)) break;
+            if (s > 1 && (f.form == k256x192 || 2 * s > KB || all > kRangeTiles || parts_bytes(s, T, N) > kPartBytes)) break;
             const int64_t each = (all + 255) / 256;   // of a CU
             const double turns = f.two > 0 ? (double)(each / 2) * f.two + (double)(each % 2) * f.one
                                            : (double)each * f.one;
             const double on = f.on * (double)((f.two > 0 ? (each + 1) / 2 : each) - 1);
             double us = std::max(cdiv(KB, s) * turns + on, bytes / 5.0e6) + f.launch;
-            if (s > 1) us += 2.5 + 0.2 * s + 8.0 * s * T * N / 4.6e6;
+            if (s > 1) us += 2.8 + 0.19 * s + 8.0 * s * T * N / 5.5e6;
             if (us < least) least = us, best = Cut{f.form, s};
         }
     }
@@ -259,10 +270,18 @@ hipError_t launch_gemm(const Product &p, Cut c, hipStream_t st) {
         case k64x32: e = launch_tiles<F32, 64, 32, 4, 1, 128, 6>(p, c.ranges, st); break;
         case k64x64: e = launch_tiles<F32, 64, 64, 4, 1, 128, 4>(p, c.ranges, st); break;
         case k128x64: e = launch_tiles<F32, 128, 64, 4, 1, 128, 3>(p, c.ranges, st); break;
+        case k128x96: e = launch_tiles<F32, 128, 96, 4, 2, 128, 4>(p, c.ranges, st); break;
         case k128x128: e = launch_tiles<F32, 128, 128, 4, 2, 128, 4>(p, c.ranges, st); break;
+        case k128x160:   // one tile of tokens: a wave's sixteen weight rows against all of them
+                         // (137 x 4096 x 14336 in eight ranges: 18.9 us, by 4 x 2 waves 20.2)
+            e = p.T <= 160 ? launch_tiles<F32, 128, 160, 8, 1, 128, 4>(p, c.ranges, st)
+                           : launch_tiles<F32, 128, 160, 4, 2, 128, 4>(p, c.ranges, st);
+            break;
         case k256x128: e = launch_tiles<F32, 256, 128, 4, 2, 128, 3>(p, c.ranges, st); break;
-        // (fp32 results of such tiles would spill registers)
-        case k256x192: e = launch_tiles<F32, 256, F32 ? 128 : 192, 4, 2, 128, F32 ? 3 : 2>(p, c.ranges, st); break;
+        case k256x192:   // (fp32 results of such tiles would spill registers: not chosen)
+            if constexpr (!F32) e = launch_tiles<F32, 256, 192, 4, 2, 128, 2>(p, c.ranges, st);
+            else e = hipErrorInvalidValue;
+            break;
     }
     if (e != hipSuccess || c.ranges == 1 || (e = hipGetLastError()) != hipSuccess) return e;
     const int64_t n = (int64_t)p.T * (p.part_pitch / 4);
@@ -347,7 +366,7 @@ int echo_int8_gemm(const int8_t *x, const float *x_scale, const int8_t *w, const
     const uintptr_t ya = (uintptr_t)y | (uintptr_t)residual;
     if (((uintptr_t)x_scale | (uintptr_t)w_scale | (uintptr_t)bias) & 3u || ya & (y_dtype == ECHO_F32 ? 3u : 1u))
         return fail(ECHO_E_INVALID, "scales, bias, y and residual must have their types' alignment");
-    const Cut cut = cut_of(num_tokens, out_features, in_features);
+    const Cut cut = cut_of(num_tokens, out_features, in_features, y_dtype == ECHO_F32);
     const size_t need = most_parts_bytes(num_tokens, out_features, in_features);
     if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u)))
         return fail(ECHO_E_WORKSPACE, "workspace of %zu bytes (need %zu, 256-byte aligned)",

@@ -42,6 +42,9 @@ __device__ __forceinline__ void landed_but_stages(int left) {
     }
 }
 
+// Scales and bias of a tile in LDS, in whole copies of 64
+constexpr int scale_room(int BN, int BT) { return (2 * BN + BT + 63) / 64 * 64; }
+
 // One workgroup of WN x WT waves: BN weight rows by BT tokens, K in steps of STEP (64
 // or 128) through a ring of S LDS stages that are filled straight from memory.  A row's
 // 16-byte pieces lie in an order that turns with the row, so that the lanes that read
@@ -63,6 +66,7 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
     // and Q lanes of a row
     constexpr int E = F32 ? 4 : 8, ROOM = STAGE / W;
     constexpr int CP = NW % 64 == 0 && ROOM >= 4096 ? 64 : NW % 32 == 0 ? 32 : 16;
+    constexpr bool CUTS = BN * BT <= 128 * 256;   // larger tiles have no registers for it
     constexpr int Q = CP / E, ROWS = Q < 4 ? 64 / Q : 16, CHUNKS = CP / 4;
     static_assert(!ONCE || BN / RC % W == 0, "a copy is of weights in all waves or none");
     static_assert(STAGE % 1024 == 0 && BN % RC == 0 && NW % CP == 0 && TW % ROWS == 0 && S >= 2);
@@ -118,7 +122,7 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
     // The scales of a tile's rows and tokens and its bias go to LDS ahead of its first
     // stage, so that nothing that is loaded stands between the results' stores.  Two
     // tiles take turns.
-    constexpr int SCALES = 2 * BN + BT, SCALE_COPIES = (SCALES + 64 * W - 1) / (64 * W);
+    constexpr int SCALES = scale_room(BN, BT), SCALE_COPIES = (SCALES + 64 * W - 1) / (64 * W);
     static_assert(BN % 64 == 0, "a copy is of one kind");
     int side = 0;
     auto copy_scales = [&] {
@@ -201,9 +205,11 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
 #pragma unroll
                         for (int k = i * COPIES / NI; k < (i + 1) * COPIES / NI; ++k)
                             if (more_k) copy(ahead, now, k);
-                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // LDS reads
-                        __builtin_amdgcn_sched_group_barrier(0x008, NJ, 0);  // matrix instructions
-                        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);   // copies
+                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);            // LDS reads
+                        __builtin_amdgcn_sched_group_barrier(0x008, NJ / 2, 0);       // matrix instructions
+                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x008, NJ - NJ / 2, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);            // copies
                     }
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) x[j] = then[j];
@@ -227,19 +233,7 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
             take(unit);
             start();
         }
-        if (u.ranges > 1) {
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const int r = wt * TW + 16 * j + c;
-                if (r >= rows_) continue;
-                int32_t *to = p.part + (range_ * (int64_t)p.T + row0_ + r) * p.part_pitch;
-#pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const int n = n0_ + wn * NW + 16 * i + 4 * g;
-                    if (n < p.part_pitch) *(i32x4 *)(to + n) = acc[i][j];
-                }
-            }
-        } else if (busy) {
+        if (busy) {
             // Sums leave through LDS, so that a store instruction writes whole pieces of rows:
             // the tile has them by columns, four of a row a lane.  A row's 16-byte chunks
             // lie in an order that turns with the row.
@@ -248,6 +242,7 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
 #pragma unroll
             for (int i0 = 0; i0 < NI; i0 += CP / 16) {
                 const int col = wn * NW + 16 * i0 + E * q, n = n0_ + col;
+                int32_t *part = p.part + (range_ * (int64_t)p.T + row0_) * p.part_pitch + n;
                 Columns<E> cols;
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
@@ -274,6 +269,14 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
 #pragma unroll
                             for (int k = 0; k < 4; ++k) sum[e + k] = s[k];
                         }
+                        if (CUTS && u.ranges > 1) {
+#pragma unroll
+                            for (int e = 0; e < E; e += 4)
+                                if (row < rows_ && n + e < p.part_pitch)
+                                    *(i32x4 *)(part + row * (int64_t)p.part_pitch + e) =
+                                        (i32x4){sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
+                            continue;
+                        }
                         float v[E];
                         cols.apply(p, sum, split(scales[2 * BN + row]), v);
                         if (row < rows_ && n < p.N) put<F32, E, (BN * BT > 128 * 256)>(p, row0_ + row, n, v);
@@ -288,7 +291,7 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
 
 template <bool F32, bool ONCE, int BN, int BT, int WN, int WT, int STEP, int S>
 hipError_t launch_tiled(const Product &p, int ranges, hipStream_t st) {
-    constexpr int bytes = S * (BN + BT) * STEP + 8 * (2 * BN + BT);
+    constexpr int bytes = S * (BN + BT) * STEP + 8 * scale_room(BN, BT);
     static_assert(bytes <= 160 * 1024);
     static std::atomic<int> resident[64];
     Units u;
