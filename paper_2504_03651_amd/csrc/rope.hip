@@ -27,6 +27,7 @@ struct Args {
     const int32_t *pos;
     int tokens, D, R;
     int per_head;               // items of a head: R / 2P that turn, then copies
+    int step_t, step_h, step_it;   // of the items that a workgroup's threads take at a time
     float magnitude, sign;
 };
 
@@ -98,16 +99,23 @@ __global__ __launch_bounds__(256) void rotate_kernel(Args a, int each, int parts
         turns[i] = turn_of(a.pos[t0 + t], a.freq[i - t * half], a.magnitude, a.sign);
     }
     __syncthreads();
-    const int items = a.heads * a.per_head, all = tokens * items, turning = half / P;
-    for (int i = part * 256 + threadIdx.x; i < all; i += 256 * parts) {
-        const int t = i / items, hi = i - t * items;
-        int h = hi / a.per_head;
-        const int it = hi - h * a.per_head;
+    // A thread's items are a fixed number of tokens, heads and items of a head apart:
+    // adding those with carries takes the place of two divisions an item (1,531 tokens
+    // of 30 heads of 80, fp32: 8.2 us with them, 7.5 without)
+    const int turning = half / P;
+    int t = 0, h, it;
+    {
+        const int i = part * 256 + threadIdx.x, hi = i / a.per_head;
+        it = i - hi * a.per_head;
+        t = hi / a.heads;
+        h = hi - t * a.heads;
+    }
+    while (t < tokens) {
         const bool second = h >= a.t[0].heads;
         const Tensor &x = second ? a.t[1] : a.t[0];
-        if (second) h -= a.t[0].heads;
-        const uint8_t *in = x.in + ((int64_t)(t0 + t) * x.in_token + h * x.in_head) * B;
-        uint8_t *out = x.out + ((int64_t)(t0 + t) * x.out_token + h * x.out_head) * B;
+        const int64_t head = second ? h - a.t[0].heads : h;
+        const uint8_t *in = x.in + ((int64_t)(t0 + t) * x.in_token + head * x.in_head) * B;
+        uint8_t *out = x.out + ((int64_t)(t0 + t) * x.out_token + head * x.out_head) * B;
         if (it < turning) {
             const float2 *w = turns + t * half + P * it;
             const int lo = INTER ? 2 * P * it : P * it, hi = INTER ? lo + P : lo + half;
@@ -147,6 +155,11 @@ __global__ __launch_bounds__(256) void rotate_kernel(Args a, int each, int parts
             u.store(out + col * B);
             if (two) v.store(out + (col + P) * B);
         }
+        it += a.step_it;
+        h += a.step_h;
+        t += a.step_t;
+        if (it >= a.per_head) it -= a.per_head, ++h;
+        if (h >= a.heads) h -= a.heads, ++t;
     }
 }
 
@@ -162,6 +175,10 @@ hipError_t launch(Args a, hipStream_t st) {
         a.tokens = (int)std::min<int64_t>(left, (int64_t)kMost * each);
         const int groups = cdiv(a.tokens, each);
         const int parts = std::max(1, std::min(cdiv((int64_t)items * each, 256), 1024 / groups));
+        const int step = 256 * parts;
+        a.step_it = step % a.per_head;
+        a.step_h = step / a.per_head % a.heads;
+        a.step_t = step / a.per_head / a.heads;
         hipLaunchKernelGGL((rotate_kernel<F32, INTER, P>), dim3((unsigned)(groups * parts)), dim3(256),
                            each * half * sizeof(float2), st, a, each, parts);
         const hipError_t e = hipGetLastError();
