@@ -20,6 +20,9 @@ using fp8::f32x4;
 using fp8::u32x2;
 using fp8::u32x4;
 
+// Codes of up to so many rows take a row by more waves of fewer values each, which has
+// the shorter way (8 rows of 4096: 5.4 us, by half the waves 7.4); past them what a wave
+// does once for its values weighs more (4,640 rows: 49 and 41 us).
 constexpr int kFewRows = 512;
 
 struct Rows {
@@ -179,12 +182,17 @@ __device__ __forceinline__ double inverse_root(double x) {
 }
 
 // A row for WAVES waves (1: four rows a workgroup), V times eight values a lane, held
-// in registers from the first step to the last.  T: what sums and rows are held in.
+// in registers from the first step to the last: one pass over memory, which bounds rows
+// in fp32 (1,003 rows of 2730, layer norms, 38 MB: 9.7 us, 4.0 TB/s, four sums one after
+// the other on the way).  Rows that end in codes are bound by instructions as well, some
+// 24 in fp64 a value: 4,640 rows of 4096 with a gate, 133 MB, take 31.4 us, 4.2 TB/s, the
+// vector units busy two thirds of it.  LEAN: two RMS norms with weights and nothing else
+// (4,640 rows: 41 us without, branches and copies of registers between them).  T: what sums and rows are held in.
 // The last eight of a row begin at H - 8, whatever H is a multiple of: what a lane
 // before them has too counts for that one alone (`skip`), and comes out the same, to be
 // written twice.  In rows of whole eights lanes behind the end hold zeros.  Where V <= 2 every input is asked for before the first sum.
 template <typename T, int WAVES, int V, bool BF, Width W, bool LEAN>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Args a, uint32_t first) {
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V == 1 && (BF || WAVES < 8) ? 8 : 1) void join_kernel(Args a, uint32_t first) {
     if (LEAN) {
         a.post = a.pre = ECHO_NORM_RMS;
         a.post_b = a.pre_b = nullptr;
@@ -466,6 +474,7 @@ template <typename T, bool BF, Width W>
 hipError_t launch_by_width(const Args &a, hipStream_t st) {
     if (a.H <= 512) return launch<T, 1, 1, BF, W>(a, st);
     if (a.H <= 2048) return launch<T, 4, 1, BF, W>(a, st);
+    if (a.H <= 6 * 512 && (sizeof(T) == 4 || a.rows <= kFewRows)) return launch<T, 6, 1, BF, W>(a, st);
     if (a.H <= 4096) {
         if constexpr (sizeof(T) == 8)
             if (a.rows > kFewRows) return launch<T, 4, 2, BF, W>(a, st);
