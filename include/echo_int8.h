@@ -32,8 +32,8 @@ extern "C" {
  *           integer (ties to even), within +-127.
  * A row with a NaN or an infinity has the scale NaN and codes of 0, so that all
  * that is computed from it is NaN.
- * codes: [rows][cols]; scales: [rows].  cols a multiple of 16; x and codes 16-byte
- * aligned, and x_stride >= cols with rows at 16-byte steps.  The buffers do not
+ * codes: [rows][cols]; scales: [rows].  cols a multiple of 16, at most 2^30; x and codes
+ * 16-byte aligned, and x_stride >= cols with rows at 16-byte steps.  The buffers do not
  * overlap. */
 int echo_int8_quantize(const void *x, int32_t x_dtype, int64_t x_stride, int32_t rows,
                        int32_t cols, int8_t *codes, float *scales, void *stream);

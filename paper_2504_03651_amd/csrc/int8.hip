@@ -324,6 +324,7 @@ int echo_int8_quantize(const void *x, int32_t x_dtype, int64_t x_stride, int32_t
         return fail(ECHO_E_UNSUPPORTED, "dtype %d of x", x_dtype);
     if (rows < 0 || cols <= 0) return fail(ECHO_E_INVALID, "rows %d, cols %d", rows, cols);
     if (cols % 16) return fail(ECHO_E_UNSUPPORTED, "cols %d is not a multiple of 16", cols);
+    if (cols > 1 << 30) return fail(ECHO_E_UNSUPPORTED, "cols %d above 2^30", cols);
     if (rows == 0) return ECHO_OK;
     const int size = x_dtype == ECHO_F32 ? 4 : 2;
     if (!x || !codes || !scales) return fail(ECHO_E_INVALID, "x, codes or scales is NULL");

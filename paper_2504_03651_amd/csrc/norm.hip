@@ -459,11 +459,12 @@ template <typename T, int WAVES, int V, bool BF, Width W, bool LEAN = false>
 hipError_t launch(const Args &a, hipStream_t st) {
     if constexpr (!LEAN && BF && W == Width::Whole && V <= 2)
         if (lean(a)) return launch<T, WAVES, V, BF, W, true>(a, st);
-    constexpr int64_t kMost = 1 << 22;   // a launch has fewer than 2^32 threads
+    constexpr int kThreads = WAVES == 1 ? 256 : 64 * WAVES;
+    constexpr int64_t kMost = ((int64_t)1 << 31) / kThreads;   // a launch has fewer than 2^32 threads
     const int64_t grid = WAVES == 1 ? ((int64_t)a.rows + 3) / 4 : a.rows;
     for (int64_t first = 0; first < grid; first += kMost) {
         hipLaunchKernelGGL((join_kernel<T, WAVES, V, BF, W, LEAN>), dim3((unsigned)std::min(kMost, grid - first)),
-                           dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, st, a, (uint32_t)first);
+                           dim3(kThreads), 0, st, a, (uint32_t)first);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

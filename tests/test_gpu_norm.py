@@ -184,7 +184,7 @@ def test_a_rows_results_are_the_same_in_any_batch():
             assert torch.equal(s2, s[at:at + T]) and torch.equal(y2, y[at:at + T])
 
 
-@pytest.mark.parametrize("T, H", [(2 ** 24 + 5, 8), (2 ** 22 + 3, 520)])
+@pytest.mark.parametrize("T, H", [(2 ** 25 + 5, 8), (2 ** 23 + 3, 520)])
 def test_more_rows_than_a_launch_holds(T, H):
     import torch
     from paper_2504_03651_amd import norm
@@ -195,6 +195,23 @@ def test_more_rows_than_a_launch_holds(T, H):
     norm.join(norm.Norm(H), None, x, y=c, y_scale=s)
     assert torch.equal(s, (x[:, 1].double() / 127).float())
     assert (c[:, 1] == 127).all() and c.count_nonzero() == T
+
+
+def test_more_long_rows_than_a_launch_holds():
+    """Rows of sixteen waves: 2^21 of them a launch."""
+    import torch
+    from paper_2504_03651_amd import norm
+    T, H = 2 ** 21 + 3, 16392
+    say(f"[case] norm of {T} rows of {H}")
+    x = torch.zeros(T, H, dtype=torch.bfloat16, device="cuda")
+    x[:, 1] = 1 + (torch.arange(T, device="cuda") % 5).bfloat16()
+    norm.join(norm.Norm(H, pre="rms", pre_eps=0.0), None, x, y=x)
+    # one value alone: the root of H, half a step of bf16 off
+    assert ((x[:, 1].float() - H ** 0.5).abs() <= 2.0 ** -8 * H ** 0.5).all()
+    for part in x.split(2 ** 16):
+        assert part.count_nonzero() == len(part)
+    del x, part
+    torch.cuda.empty_cache()
 
 
 def test_no_rows_and_refusals_on_the_gpu():

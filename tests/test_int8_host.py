@@ -66,7 +66,8 @@ QUANT = dict(x=P, dtype=0, stride=256, rows=4, cols=256, codes=P, scales=P)
 @pytest.mark.parametrize("change, code, what", [
     (dict(x=None), INV, "NULL"), (dict(codes=None), INV, "NULL"), (dict(scales=None), INV, "NULL"),
     (dict(dtype=2), UNS, "dtype"), (dict(rows=-1), INV, "rows"), (dict(cols=0), INV, "cols"),
-    (dict(cols=250), UNS, "multiple of 16"), (dict(stride=240), INV, "x_stride"),
+    (dict(cols=250), UNS, "multiple of 16"), (dict(cols=2 ** 30 + 16, stride=2 ** 31), UNS, "above"),
+    (dict(stride=240), INV, "x_stride"),
     (dict(stride=260), INV, "x_stride"), (dict(dtype=1, stride=258), INV, "x_stride"),
     (dict(x=at(8)), INV, "aligned"), (dict(codes=at(8)), INV, "aligned"), (dict(scales=at(2)), INV, "aligned"),
 ])
