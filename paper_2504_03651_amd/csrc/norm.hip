@@ -471,16 +471,24 @@ hipError_t launch(const Args &a, hipStream_t st) {
     return hipSuccess;
 }
 
+// Sums in fp32 depend on how a row is spread over lanes, so that this goes by its width
+// alone; codes, which do not, take fewer waves of more values each where rows are many
+// (4,333 rows of 640: 11.8 us by one wave, by four of which a row fills a third 16.3).
+// Sixteen waves a row of up to 8192 were slower than eight (12 rows of 5264 5.8 and 5.2
+// us, 1,136 of 7062 in fp32 37.6 and 33.1).
 template <typename T, bool BF, Width W>
 hipError_t launch_by_width(const Args &a, hipStream_t st) {
     if (a.H <= 512) return launch<T, 1, 1, BF, W>(a, st);
+    if constexpr (sizeof(T) == 8)
+        if (a.rows > kFewRows) {
+            if (a.H <= 1024) return launch<T, 1, 2, BF, W>(a, st);
+            if (a.H <= 2048) return launch<T, 2, 2, BF, W>(a, st);
+            if (a.H <= 4096) return launch<T, 4, 2, BF, W>(a, st);
+        }
+    if (a.H <= 1024) return launch<T, 2, 1, BF, W>(a, st);
     if (a.H <= 2048) return launch<T, 4, 1, BF, W>(a, st);
-    if (a.H <= 6 * 512 && (sizeof(T) == 4 || a.rows <= kFewRows)) return launch<T, 6, 1, BF, W>(a, st);
-    if (a.H <= 4096) {
-        if constexpr (sizeof(T) == 8)
-            if (a.rows > kFewRows) return launch<T, 4, 2, BF, W>(a, st);
-        return launch<T, 8, 1, BF, W>(a, st);
-    }
+    if (a.H <= 6 * 512) return launch<T, 6, 1, BF, W>(a, st);
+    if (a.H <= 4096) return launch<T, 8, 1, BF, W>(a, st);
     if (a.H <= 8192) return launch<T, 8, 2, BF, W>(a, st);
     if (a.H <= 16384) return launch<T, 8, 4, BF, W>(a, st);
     if constexpr (sizeof(T) == 4) return launch<T, 16, 4, BF, W>(a, st);
