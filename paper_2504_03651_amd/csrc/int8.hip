@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256) void add_parts_kernel(Product p, int ranges) {
     const int sum[4] = {s[0], s[1], s[2], s[3]};
     float v[4];
     cols.apply(p, sum, xs, v);
-    put<F32, 4>(p, t, n, v);
+    put_sum<F32, 4>(p, t, n, v);
 }
 
 // stages of a wave's ring, for NT = 1 and 2: at most 160 KiB for eight waves
@@ -161,7 +161,7 @@ constexpr int rows_depth(int NT, int XR) { return std::min(6, 160 * 1024 / (kStr
 constexpr int rows_tokens(int T) { return T <= 8 ? 8 : T <= 16 ? 16 : 32; }
 
 // How a product is cut: the kernel's form, and how many ranges of K there are.
-enum Form { kRows16, kRows32, k64x32, k64x64, k128x64, k128x96, k128x128, k128x160, k256x128, k256x192 };
+enum Form { kRows16, kRows32, k64x32, k64x64, k128x64, k128x96, k128x128, k128x128two, k128x160, k256x128, k256x192 };
 struct Cut {
     Form form;
     int ranges;
@@ -173,10 +173,11 @@ constexpr struct {
     Form form;
     int n, t;
     double one, two, launch, on;
-} kTileForms[] = {{k64x32, 64, 32, .25, .41, 3.1, 2.},   {k64x64, 64, 64, .36, .42, 3.5, 2.},
-                  {k128x64, 128, 64, .54, .75, 3.3, 2.}, {k128x96, 128, 96, .57, 0, 3.3, 2.},
-                  {k128x128, 128, 128, .59, 0, 3.5, 2.},   {k128x160, 128, 160, .67, 0, 3.5, 2.},
-                  {k256x128, 256, 128, .77, 0, 3.5, 2.}, {k256x192, 256, 192, 1.16, 0, 4., 3.1}};
+} kTileForms[] = {{k64x32, 64, 32, .25, .42, 3.1, 2.},       {k64x64, 64, 64, .27, .41, 3.8, 2.},
+                  {k128x64, 128, 64, .54, .75, 3.75, 2.},    {k128x96, 128, 96, .53, 0, 3.7, 2.},
+                  {k128x128, 128, 128, .59, 0, 3.75, 2.},    {k128x128two, 128, 128, .70, .85, 3.55, 1.7},
+                  {k128x160, 128, 160, .72, 0, 3.5, 2.},     {k256x128, 256, 128, .77, 0, 3.7, 2.},
+                  {k256x192, 256, 192, 1.15, 0, 4., 3.4}};
 constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16};
 
 // Products of more tiles, or whose parts would take more, are not cut into ranges of K,
@@ -204,14 +205,18 @@ size_t most_parts_bytes(int T, int N, int K) {
 }
 
 // The cut of least estimated time, in microseconds fitted to bf16 results of 430 sizes (T 1
-// to 4,640, N 64 to 28,672, K 128 to 14,336, weights from memory): 0.7% (geometric mean)
-// above the best cut of each, 23% at most (20 x 17342 x 8256, where four ranges of K would
-// be best); over 130 sizes with fp32 results 0.7% and 21%.
+// to 4,640, N 64 to 28,672, K 128 to 14,336, weights from memory): 1.0% (geometric mean)
+// above the best cut of each, 24% at most (20 x 17342 x 8256, where four ranges of K would
+// be best); over 130 sizes with fp32 results 1.2% and 35% (54 x 5152 x 8080).
 //   Weights and tokens come at 5.0 TB/s at most.
 //   kRows: 16 or 32 weight rows a workgroup, every wave on its own; one workgroup a
 //   CU, which takes in 70 KB a microsecond, tokens among them (8 x 6144 x 4096: 7.2 by 32
 //   rows; 64 x 32 tiles take over where a CU has more than one: 8 x 10911 x 3056 14.4
 //   and 11.7).
+//   k128x128two: four waves of 64 x 64, two workgroups a CU, so that one's results leave
+//   beside the other's products (1,847 x 26626 x 512 55 us, in tiles of 256 x 192 76, of
+//   128 x 128 by eight waves, four stages and one workgroup a CU, which ranges of K and
+//   few tiles take, 78).
 //   Ranges of K cost a second launch and their sums' way to memory and back.
 Cut cut_of(int T, int N, int K, bool f32) {
     const int KB = cdiv(K, kStep);
@@ -227,16 +232,17 @@ Cut cut_of(int T, int N, int K, bool f32) {
         if (us < least) least = us, best = Cut{nt == 1 ? kRows16 : kRows32, 1};
     }
     for (const auto &f : kTileForms) {
-        if ((f.t > 32 && T <= f.t / 3) || (f32 && f.form == k256x192)) continue;
+        if ((f.t > 32 && T <= f.t / 3) || (f32 && (f.form == k128x128two || f.form == k256x192))) continue;
         for (int s : kRanges) {
             const int64_t all = (int64_t)cdiv(N, f.n) * cdiv(T, f.t) * s;
             if (s > 1 && (f.form == k256x192 || 2 * s > KB || all > kRangeTiles || parts_bytes(s, T, N) > kPartBytes)) break;
             const int64_t each = (all + 255) / 256;   // of a CU
-            const double turns = f.two > 0 ? (double)(each / 2) * f.two + (double)(each % 2) * f.one
-                                           : (double)each * f.one;
+            const double one = f.form == k128x160 && T <= 160 ? .62 : f.one;   // waves of 16 x 160
+            const double turns = f.two > 0 ? (double)(each / 2) * f.two + (double)(each % 2) * one
+                                           : (double)each * one;
             const double on = f.on * (double)((f.two > 0 ? (each + 1) / 2 : each) - 1);
             double us = std::max(cdiv(KB, s) * turns + on, bytes / 5.0e6) + f.launch;
-            if (s > 1) us += 2.8 + 0.19 * s + 8.0 * s * T * N / 5.5e6;
+            if (s > 1) us += 2.6 + 0.19 * s + 8.0 * s * T * N / 5.0e6;
             if (us < least) least = us, best = Cut{f.form, s};
         }
     }
@@ -278,10 +284,10 @@ hipError_t launch_gemm(const Product &p, Cut c, hipStream_t st) {
                            : launch_tiles<F32, 128, 160, 4, 2, 128, 4>(p, c.ranges, st);
             break;
         case k256x128: e = launch_tiles<F32, 256, 128, 4, 2, 128, 3>(p, c.ranges, st); break;
-        case k256x192:   // (fp32 results of such tiles would spill registers: not chosen)
-            if constexpr (!F32) e = launch_tiles<F32, 256, 192, 4, 2, 128, 2>(p, c.ranges, st);
-            else e = hipErrorInvalidValue;
-            break;
+        default:   // fp32 results of these tiles would spill registers: not chosen
+            if constexpr (F32) e = hipErrorInvalidValue;
+            else if (c.form == k128x128two) e = launch_tiles<F32, 128, 128, 2, 2, 128, 2>(p, c.ranges, st);
+            else e = launch_tiles<F32, 256, 192, 4, 2, 128, 2>(p, c.ranges, st);
     }
     if (e != hipSuccess || c.ranges == 1 || (e = hipGetLastError()) != hipSuccess) return e;
     const int64_t n = (int64_t)p.T * (p.part_pitch / 4);

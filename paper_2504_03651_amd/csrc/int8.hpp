@@ -61,54 +61,84 @@ __device__ __forceinline__ float scaled(int sum, Scale x, Scale w) {
     return __builtin_amdgcn_ldexpf((float)sum * x.m * w.m, x.e + w.e);
 }
 
-// E columns from n of row t, whose scaled sums with bias are v: the residual is added,
-// and y written; PAST: past the caches
+// The residual of E columns from n, at element `at`
+template <bool F32, int E>
+struct Rest {
+    static constexpr int WORDS = F32 ? E : E / 2;
+    uint32_t b[WORDS];
+    __device__ __forceinline__ void load(const Product &p, int64_t at, int n) {
+        if (n + E <= p.N) {
+            if constexpr (WORDS == 4) {
+                const u32x4 r = F32 ? __builtin_bit_cast(u32x4, *(const any_f32x4 *)((const float *)p.residual + at))
+                                    : (u32x4)*(const any_u32x4 *)((const uint16_t *)p.residual + at);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[i] = r[i];
+            } else {
+                static_assert(!F32 && WORDS == 2);
+                const u32x2 r = *(const any_u32x2 *)((const uint16_t *)p.residual + at);
+                b[0] = r[0], b[1] = r[1];
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            if constexpr (F32) {
+                b[i] = n + i < p.N ? __float_as_uint(((const float *)p.residual)[at + i]) : 0u;
+            } else {
+                const uint16_t *r = (const uint16_t *)p.residual + at + 2 * i;
+                b[i] = (n + 2 * i < p.N ? r[0] : 0u) | (n + 2 * i + 1 < p.N ? (uint32_t)r[1] << 16 : 0u);
+            }
+        }
+    }
+    __device__ __forceinline__ void add(float (&v)[E]) const {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            if constexpr (F32) v[i] += __uint_as_float(b[i]);
+            else v[2 * i] += bf2f(b[i] & 0xFFFFu), v[2 * i + 1] += bf2f(b[i] >> 16);
+        }
+    }
+};
+
+// y of E columns from n of row t; PAST: past the caches
 template <bool F32, int E, bool PAST = false>
-__device__ __forceinline__ void put(const Product &p, int64_t t, int n, float (&v)[E]) {
-    static_assert(E == 4 || E == 8);
+__device__ __forceinline__ void put(const Product &p, int64_t t, int n, const float (&v)[E]) {
+    static_assert(E == 4 || (E == 8 && !F32));
     const int64_t at = t * p.y_stride + n;
     if (n + E <= p.N) {
         if constexpr (F32) {
-#pragma unroll
-            for (int e = 0; e < E; e += 4) {
-                f32x4 o = {v[e], v[e + 1], v[e + 2], v[e + 3]};
-                if (p.residual) o += *(const any_f32x4 *)((const float *)p.residual + at + e);
-                if (PAST) __builtin_nontemporal_store(o, (any_f32x4 *)((float *)p.y + at + e));
-                else *(any_f32x4 *)((float *)p.y + at + e) = o;
-            }
+            const f32x4 o = {v[0], v[1], v[2], v[3]};
+            if (PAST) __builtin_nontemporal_store(o, (any_f32x4 *)((float *)p.y + at));
+            else *(any_f32x4 *)((float *)p.y + at) = o;
         } else {
             uint32_t o[E / 2];
-            if (p.residual) {
-                if constexpr (E == 8) {
-                    const u32x4 r = *(const any_u32x4 *)((const uint16_t *)p.residual + at);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[2 * e] += bf2f(r[e] & 0xFFFFu), v[2 * e + 1] += bf2f(r[e] >> 16);
-                } else {
-                    const u32x2 r = *(const any_u32x2 *)((const uint16_t *)p.residual + at);
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) v[2 * e] += bf2f(r[e] & 0xFFFFu), v[2 * e + 1] += bf2f(r[e] >> 16);
-                }
-            }
 #pragma unroll
             for (int e = 0; e < E / 2; ++e) o[e] = f2bf2(v[2 * e], v[2 * e + 1]);
             if constexpr (E == 8 && PAST)
                 __builtin_nontemporal_store((u32x4){o[0], o[1], o[2], o[3]}, (any_u32x4 *)((uint16_t *)p.y + at));
             else if constexpr (E == 8)
                 *(any_u32x4 *)((uint16_t *)p.y + at) = (u32x4){o[0], o[1], o[2], o[3]};
-            else *(any_u32x2 *)((uint16_t *)p.y + at) = (u32x2){o[0], o[1]};
+            else
+                *(any_u32x2 *)((uint16_t *)p.y + at) = (u32x2){o[0], o[1]};
         }
         return;
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         if (n + e >= p.N) continue;
-        if constexpr (F32) {
-            ((float *)p.y)[at + e] = v[e] + (p.residual ? ((const float *)p.residual)[at + e] : 0.f);
-        } else {
-            const float r = p.residual ? bf2f(((const uint16_t *)p.residual)[at + e]) : 0.f;
-            ((uint16_t *)p.y)[at + e] = (uint16_t)f2bf(v[e] + r);
-        }
+        if constexpr (F32) ((float *)p.y)[at + e] = v[e];
+        else ((uint16_t *)p.y)[at + e] = (uint16_t)f2bf(v[e]);
     }
+}
+
+// the same with the residual, if any
+template <bool F32, int E, bool PAST = false>
+__device__ __forceinline__ void put_sum(const Product &p, int64_t t, int n, float (&v)[E]) {
+    if (p.residual) {
+        Rest<F32, E> r;
+        r.load(p, t * p.y_stride + n, n);
+        r.add(v);
+    }
+    put<F32, E, PAST>(p, t, n, v);
 }
 
 // Scales and bias of E columns from n

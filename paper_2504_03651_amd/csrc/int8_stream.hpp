@@ -101,7 +101,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void stream_kernel(Product p, in
             const int sum[4] = {s[0], s[1], s[2], s[3]};
             float v[4];
             cols.apply(p, sum, split(p.xs[row0 + r]), v);
-            put<F32, 4>(p, row0 + r, n, v);
+            put_sum<F32, 4>(p, row0 + r, n, v);
         }
     }
 }

@@ -45,6 +45,9 @@ __device__ __forceinline__ void landed_but_stages(int left) {
 // Scales and bias of a tile in LDS, in whole copies of 64
 constexpr int scale_room(int BN, int BT) { return (2 * BN + BT + 63) / 64 * 64; }
 
+// LDS of a workgroup: two share a CU where it holds them
+constexpr int lds_bytes(int BN, int BT, int STEP, int S) { return S * (BN + BT) * STEP + 8 * scale_room(BN, BT); }
+
 // One workgroup of WN x WT waves: BN weight rows by BT tokens, K in steps of STEP (64
 // or 128) through a ring of S LDS stages that are filled straight from memory.  A row's
 // 16-byte pieces lie in an order that turns with the row, so that the lanes that read
@@ -55,7 +58,7 @@ constexpr int scale_room(int BN, int BT) { return (2 * BN + BT + 63) / 64 * 64; 
 // No more workgroups are launched than run at once: each goes on to a next tile, whose
 // first copies it starts before it writes the last one's results through one stage.
 template <bool F32, bool ONCE, int BN, int BT, int WN, int WT, int STEP, int S>
-__global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units u) {
+__global__ __launch_bounds__(64 * WN * WT, WN * WT * (2 * lds_bytes(BN, BT, STEP, S) <= 160 * 1024 ? 2 : 1) / 4) void tiled_kernel(Product p, Units u) {
     constexpr int W = WN * WT, NW = BN / WN, TW = BT / WT;   // a wave's rows and tokens
     constexpr int NI = NW / 16, NJ = TW / 16, NH = STEP / 64;
     constexpr int STAGE = (BN + BT) * STEP;
@@ -66,7 +69,9 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
     // and Q lanes of a row
     constexpr int E = F32 ? 4 : 8, ROOM = STAGE / W;
     constexpr int CP = NW % 64 == 0 && ROOM >= 4096 ? 64 : NW % 32 == 0 ? 32 : 16;
-    constexpr bool CUTS = BN * BT <= 128 * 256;   // larger tiles have no registers for it
+    // ranges of K, and a residual that is asked for early: where registers allow it
+    constexpr bool CUTS = BN * BT <= 128 * 256;
+    constexpr bool REST = BN * BT * (F32 ? 2 : 1) <= 128 * 256 && (W <= 4 || 2 * lds_bytes(BN, BT, STEP, S) > 160 * 1024);
     constexpr int Q = CP / E, ROWS = Q < 4 ? 64 / Q : 16, CHUNKS = CP / 4;
     static_assert(!ONCE || BN / RC % W == 0, "a copy is of weights in all waves or none");
     static_assert(STAGE % 1024 == 0 && BN % RC == 0 && NW % CP == 0 && TW % ROWS == 0 && S >= 2);
@@ -219,6 +224,21 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
             }
         }
 
+        // The residual is asked for ahead of the next tile's copies and of all stores, which
+        // it would wait for: memory answers in order.
+        constexpr int PARTS = NI / (CP / 16), READS = TW / (64 / Q);   // of a wave's columns, of its rows
+        Rest<F32, E> rest[REST ? PARTS : 1][REST ? READS : 1];
+        const bool early = REST && p.residual && u.ranges == 1 && busy;
+        if (early) {
+#pragma unroll
+            for (int i = 0; i < (REST ? PARTS : 1); ++i)
+#pragma unroll
+                for (int k = 0; k < (REST ? READS : 1); ++k) {
+                    const int row = wt * TW + k * (64 / Q) + lane / Q, n = n0 + wn * NW + CP * i + E * (lane % Q);
+                    if (row < rows && n < p.N) rest[i][k].load(p, (row0 + row) * p.y_stride + n, n);
+                }
+        }
+
         // the next unit's first stages go to the slots behind the one that the epilogue
         // takes, the last one read
         const int n0_ = n0, row0_ = row0, rows_ = rows, range_ = range;
@@ -279,7 +299,13 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
                         }
                         float v[E];
                         cols.apply(p, sum, split(scales[2 * BN + row]), v);
-                        if (row < rows_ && n < p.N) put<F32, E, (BN * BT > 128 * 256)>(p, row0_ + row, n, v);
+                        if (row >= rows_ || n >= p.N) continue;
+                        if constexpr (REST) {
+                            if (early) rest[i0 / (CP / 16)][(16 * j0 + r0) / (64 / Q)].add(v);
+                            put<F32, E>(p, row0_ + row, n, v);
+                        } else {
+                            put_sum<F32, E, !CUTS>(p, row0_ + row, n, v);
+                        }
                     }
                     wave_lds();
                 }
@@ -291,7 +317,7 @@ __global__ __launch_bounds__(64 * WN * WT, 1) void tiled_kernel(Product p, Units
 
 template <bool F32, bool ONCE, int BN, int BT, int WN, int WT, int STEP, int S>
 hipError_t launch_tiled(const Product &p, int ranges, hipStream_t st) {
-    constexpr int bytes = S * (BN + BT) * STEP + 8 * scale_room(BN, BT);
+    constexpr int bytes = lds_bytes(BN, BT, STEP, S);
     static_assert(bytes <= 160 * 1024);
     static std::atomic<int> resident[64];
     Units u;

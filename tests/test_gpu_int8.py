@@ -155,10 +155,11 @@ SIZES += [(34, 4185, 16), (17, 1, 11296), (34, 1, 11104), (160, 6001, 4112), (35
           (34, 4107, 5344), (132, 16617, 16), (132, 16617, 400), (33, 4131, 5680), (66, 16935, 16), (70, 16935, 656),
           (70, 5579, 3392), (203, 16699, 16), (203, 16699, 528), (133, 2713, 10192), (398, 16971, 16), (398, 16971, 656),
           (770, 19001, 272), (130, 10939, 8160), (97, 16894, 16), (98, 5449, 3552), (2713, 133, 7264), (161, 17594, 16),
-          (164, 5685, 4880)]
+          (164, 5685, 4880), (2012, 133, 12064), (98, 9651, 5792), (67, 2813, 9360), (2707, 145, 13856), (167, 17453, 288)]
 # workgroups that go on to a next tile: more tiles than run at once
 SIZES += [(40, 41003, 272), (64, 50021, 144), (190, 35003, 144), (280, 33001, 272), (1500, 8197, 144), (3001, 4099, 272),
-          (900, 28679, 272), (20, 35329, 528), (259, 43662, 272), (388, 32795, 144)]
+          (900, 28679, 272), (20, 35329, 528), (259, 43662, 272), (388, 32795, 144),
+          (193, 35673, 528), (258, 32974, 528), (261, 49271, 528)]
 
 
 @pytest.mark.parametrize("f32", [True, False])
