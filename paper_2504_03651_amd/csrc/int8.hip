@@ -19,7 +19,8 @@ namespace int8 {
 // and every scale fp32(b / 127) of a bf16 b; for fp32 values the residual is taken twice,
 // after which the quotient itself is the correctly rounded one.  Both need a scale in
 // [2^-100, 2^100]; others divide.  The quotient of a row's largest value is below 127.5
-// by far more than its rounding, so nothing needs clamping then.
+// by far more than its rounding, so nothing needs clamping then.  Bound by memory: 66.5
+// million bf16 values (4,640 rows of 14336) take 38.6 us, 5.2 TB/s; 8 fp32 rows of 4096 3.0.
 
 // Codes of four quotients, in a word: adding 1.5 * 2^23 leaves the nearest integer (ties
 // to even) in the low bits.
@@ -45,7 +46,8 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 }
 
 // A row for WAVES waves, 256 / (64 WAVES) rows a workgroup; V times eight values a lane,
-// held in registers between the search for the largest and the codes.  HELD false: rows
+// held in registers between the search for the largest and the codes, so that a row is
+// read once.  HELD false: rows
 // longer than that are read twice.
 template <bool F32, int WAVES, int V, bool HELD>
 __global__ __launch_bounds__(256) void quantize_kernel(const void *x, int64_t stride, int rows, int cols,

@@ -159,7 +159,8 @@ SIZES += [(34, 4185, 16), (17, 1, 11296), (34, 1, 11104), (160, 6001, 4112), (35
 # workgroups that go on to a next tile: more tiles than run at once
 SIZES += [(40, 41003, 272), (64, 50021, 144), (190, 35003, 144), (280, 33001, 272), (1500, 8197, 144), (3001, 4099, 272),
           (900, 28679, 272), (20, 35329, 528), (259, 43662, 272), (388, 32795, 144),
-          (193, 35673, 528), (258, 32974, 528), (261, 49271, 528)]
+          (193, 35673, 528), (258, 32974, 528), (261, 49271, 528),
+          (1545, 4963, 16), (67, 16810, 4944), (193, 36583, 272)]
 
 
 @pytest.mark.parametrize("f32", [True, False])
