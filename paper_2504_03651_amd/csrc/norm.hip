@@ -145,16 +145,20 @@ __device__ __forceinline__ double meet_rows(double v, F join) {
 
 template <typename T, int WAVES>
 struct Across {
-    T (*room)[WAVES];
+    T (*room)[2 * WAVES];
     int turn;
     template <typename F>
-    __device__ __forceinline__ T all(T v, F join) {
+    __device__ __forceinline__ T wave(T v, F join) {
         v = meet<0x128>(v, join);   // row_ror:8, 4, 2, 1
         v = meet<0x124>(v, join);
         v = meet<0x122>(v, join);
         v = meet<0x121>(v, join);
         v = meet_rows<16>(v, join);
-        v = meet_rows<32>(v, join);
+        return meet_rows<32>(v, join);
+    }
+    template <typename F>
+    __device__ __forceinline__ T all(T v, F join) {
+        v = wave(v, join);
         if constexpr (WAVES > 1) {
             T *part = room[turn];
             turn ^= 1;
@@ -166,11 +170,23 @@ struct Across {
         }
         return v;
     }
-    __device__ __forceinline__ T sum(T v) {
-        return all(v, [](T a, T b) { return a + b; });
-    }
-    __device__ __forceinline__ T max(T v) {
-        return all(v, [](T a, T b) { return a > b ? a : b; });
+    static __device__ __forceinline__ T add(T a, T b) { return a + b; }
+    static __device__ __forceinline__ T more(T a, T b) { return a > b ? a : b; }
+    __device__ __forceinline__ T sum(T v) { return all(v, add); }
+    __device__ __forceinline__ T max(T v) { return all(v, more); }
+    // the sum of s and the largest of m, behind one barrier
+    __device__ __forceinline__ void both(T &s, T &m) {
+        s = wave(s, add);
+        m = wave(m, more);
+        if constexpr (WAVES > 1) {
+            T *part = room[turn];
+            turn ^= 1;
+            if ((threadIdx.x & 63) == 0) part[2 * (threadIdx.x >> 6)] = s, part[2 * (threadIdx.x >> 6) + 1] = m;
+            __syncthreads();
+            s = part[0], m = part[1];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) s = s + part[2 * w], m = more(m, part[2 * w + 1]);
+        }
     }
 };
 
@@ -201,7 +217,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
     constexpr int LANES = 64 * WAVES;
     constexpr bool EARLY = V <= 2, TINY = W == Width::Tiny, WHOLE = W == Width::Whole;
     typedef Raw<BF, TINY> R;
-    __shared__ __align__(16) T room[2][WAVES];
+    __shared__ __align__(16) T room[2][2 * WAVES];
     Across<T, WAVES> across{room, 0};
     const int lane = threadIdx.x % LANES;
     int64_t row = WAVES == 1 ? 4 * ((int64_t)first + blockIdx.x) + threadIdx.x / 64 : (int64_t)first + blockIdx.x;
@@ -250,9 +266,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
     };
 
     T x[V][8];
-    // x less its mean (LAYER) and 1 / sqrt(mean of squares + eps).  The sum is divided by H
-    // exactly enough that a row of one value has that for its mean.
-    auto inverse = [&](int kind, float eps) {
+    // x less its mean (LAYER).  The sum is divided by H exactly enough that a row of one
+    // value has that for its mean.
+    auto centre = [&](int kind) {
         if (kind == ECHO_NORM_LAYER) {
             T s = T(0);
 #pragma unroll
@@ -268,13 +284,16 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[u][i] = behind(u) ? T(0) : x[u][i] - mean;
         }
+    };
+    auto squares = [&] {   // of this lane
         T ss = T(0);
 #pragma unroll
         for (int u = 0; u < V; ++u)
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss = fma(x[u][i], mine(u, i) ? x[u][i] : T(0), ss);
-        return inverse_root(fma(across.sum(ss), (T)a.inv_h, (T)eps));
+        return ss;
     };
+    auto inverse = [&](T ss, float eps) { return inverse_root(fma(ss, (T)a.inv_h, (T)eps)); };
     const T offset = (T)a.weight_offset;
     auto weigh = [&](int u, const R &w) {
         if (a.weight_offset == 0.f) {
@@ -296,7 +315,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
         }
         T by = (T)a.block_scale;
         if (a.post != ECHO_NORM_NONE) {
-            const T inv = inverse(a.post, a.post_eps);
+            centre(a.post);
+            const T inv = inverse(across.sum(squares()), a.post_eps);
             if (post_w) {
 #pragma unroll
                 for (int u = 0; u < V; ++u) {
@@ -357,25 +377,54 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
         }
     }
     if (!y) return;
-    T inv = T(1);
-    if (a.pre != ECHO_NORM_NONE) {
-        inv = inverse(a.pre, a.pre_eps);
-        if (pre_w) {
+    // The largest of y, where that is codes, is the largest of x times 1 / root, so that it
+    // is looked for along with the squares' sum, but under a bias.
+    T inv = T(1), top = T(0);
+    auto largest = [&] {   // of this lane: infinite where an infinity or a NaN is
+        T top = T(0), odds = T(0);
 #pragma unroll
-            for (int u = 0; u < V; ++u) {
-                apart();
-                weigh(u, EARLY ? rw2[EARLY ? u : 0] : param(a.pre_w, u));
+        for (int u = 0; u < V; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (TINY && !mine(u, i)) continue;
+                top = fmax(top, fabs(x[u][i]));
+                odds = fma(x[u][i], T(0), odds);   // 0, or NaN
             }
+        return odds == T(0) ? top : (T)INFINITY;
+    };
+    constexpr bool CODES = sizeof(T) == 8;
+    const bool normed = a.pre != ECHO_NORM_NONE;
+    if (normed) centre(a.pre);
+    T ss = normed ? squares() : T(0);
+    if (CODES ? a.pre_b != nullptr : normed) {
+        ss = across.sum(ss);
+        inv = inverse(ss, a.pre_eps);
+    }
+    if (pre_w && normed) {
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+            apart();
+            weigh(u, EARLY ? rw2[EARLY ? u : 0] : param(a.pre_w, u));
         }
+    }
+    if (a.pre_b) {   // (none where there is no norm)
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+            apart();
+            const R w = param(a.pre_b, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[u][i] = behind(u) ? T(0) : fma(x[u][i], inv, (T)w.get(a.param_f32, i));
+        }
+        inv = T(1);
+    }
+    if constexpr (CODES) {
+        top = largest();
         if (a.pre_b) {
-#pragma unroll
-            for (int u = 0; u < V; ++u) {
-                apart();
-                const R w = param(a.pre_b, u);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[u][i] = behind(u) ? T(0) : fma(x[u][i], inv, (T)w.get(a.param_f32, i));
-            }
-            inv = T(1);
+            top = across.max(top);
+        } else {
+            across.both(ss, top);
+            if (normed) inv = inverse(ss, a.pre_eps);
+            top *= inv;
         }
     }
     if constexpr (sizeof(T) == 4) {
@@ -388,17 +437,6 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
             if (skip[u] < 8) store8<BF, TINY>(a.y.data, a.y.f32, row * a.y.stride + col[u], n, f);
         }
     } else {
-        // y is x inv; the largest of one is the largest of the other's
-        T top = T(0), odds = T(0);   // odds: 0, or NaN where an infinity or a NaN is
-#pragma unroll
-        for (int u = 0; u < V; ++u)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (TINY && !mine(u, i)) continue;
-                top = fmax(top, fabs(x[u][i]));
-                odds = fma(x[u][i], T(0), odds);
-            }
-        top = across.max(odds == T(0) ? top : (T)INFINITY) * inv;
         // top / 127, its product with 1 / 127 corrected by the residual
         constexpr double k127 = 1.0 / 127.0;
         const T part = top * k127;
