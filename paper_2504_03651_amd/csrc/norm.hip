@@ -41,6 +41,9 @@ struct Args {
     int rows, in_place;
 };
 
+// Pairs of norms that have a form of their own, without the branches for all the others
+enum class Lean { No, Rms, Layer };
+
 // Rows of whole eights, of any other width, and those shorter than eight
 enum class Width { Whole, Odd, Tiny };
 
@@ -202,16 +205,18 @@ __device__ __forceinline__ double inverse_root(double x) {
 // in fp32 (1,003 rows of 2730, layer norms, 38 MB: 9.7 us, 4.0 TB/s, four sums one after
 // the other on the way).  Rows that end in codes are bound by instructions as well, some
 // 24 in fp64 a value: 4,640 rows of 4096 with a gate, 133 MB, take 31.4 us, 4.2 TB/s, the
-// vector units busy two thirds of it.  LEAN: two RMS norms with weights and nothing else
-// (4,640 rows: 41 us without, branches and copies of registers between them).  T: what sums and rows are held in.
+// vector units busy two thirds of it.  LEAN: two RMS norms with weights, or two LAYER
+// norms with weights and biases, and no branches for all else, which cost copies of
+// registers between them (4,640 rows of two RMS norms: 41 us without; 3,937 of 6936 with
+// the stream in fp32 104, 73 with).  T: what sums and rows are held in.
 // The last eight of a row begin at H - 8, whatever H is a multiple of: what a lane
 // before them has too counts for that one alone (`skip`), and comes out the same, to be
 // written twice.  In rows of whole eights lanes behind the end hold zeros.  Where V <= 2 every input is asked for before the first sum.
-template <typename T, int WAVES, int V, bool BF, Width W, bool LEAN>
+template <typename T, int WAVES, int V, bool BF, Width W, Lean LEAN>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V == 1 && (BF || WAVES < 8) ? 8 : 1) void join_kernel(Args a, uint32_t first) {
-    if (LEAN) {
-        a.post = a.pre = ECHO_NORM_RMS;
-        a.post_b = a.pre_b = nullptr;
+    constexpr bool USUAL = LEAN != Lean::No;
+    if (USUAL) {
+        a.post = a.pre = LEAN == Lean::Rms ? ECHO_NORM_RMS : ECHO_NORM_LAYER;
         a.weight_offset = 0.f;
     }
     constexpr int LANES = 64 * WAVES;
@@ -246,8 +251,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
         v.load(p, a.param_f32, col[u], n);
         return v;
     };
-    const bool block = LEAN || a.block.data, gate = block && a.gate.data, residual = LEAN || a.residual.data;
-    const bool y = LEAN || a.y.data, post_w = LEAN || a.post_w, pre_w = LEAN || a.pre_w;
+    const bool block = USUAL || a.block.data, gate = block && a.gate.data, residual = USUAL || a.residual.data;
+    const bool y = USUAL || a.y.data, post_w = USUAL || a.post_w, pre_w = USUAL || a.pre_w;
+    const bool post_b = USUAL ? LEAN == Lean::Layer : a.post_b != nullptr;
+    const bool pre_b = USUAL ? LEAN == Lean::Layer : a.pre_b != nullptr;
     R rb[EARLY ? V : 1], rg[EARLY ? V : 1], rr[EARLY ? V : 1], rw[EARLY ? V : 1], rw2[EARLY ? V : 1];
     if constexpr (EARLY) {
 #pragma unroll
@@ -324,7 +331,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
                     weigh(u, EARLY ? rw[EARLY ? u : 0] : param(a.post_w, u));
                 }
             }
-            if (a.post_b) {
+            if (post_b) {
 #pragma unroll
                 for (int u = 0; u < V; ++u) {
                     apart();
@@ -396,7 +403,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
     const bool normed = a.pre != ECHO_NORM_NONE;
     if (normed) centre(a.pre);
     T ss = normed ? squares() : T(0);
-    if (CODES ? a.pre_b != nullptr : normed) {
+    if (CODES ? pre_b : normed) {
         ss = across.sum(ss);
         inv = inverse(ss, a.pre_eps);
     }
@@ -407,7 +414,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
             weigh(u, EARLY ? rw2[EARLY ? u : 0] : param(a.pre_w, u));
         }
     }
-    if (a.pre_b) {   // (none where there is no norm)
+    if (pre_b) {   // (none where there is no norm)
 #pragma unroll
         for (int u = 0; u < V; ++u) {
             apart();
@@ -419,7 +426,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
     }
     if constexpr (CODES) {
         top = largest();
-        if (a.pre_b) {
+        if (pre_b) {
             top = across.max(top);
         } else {
             across.both(ss, top);
@@ -487,16 +494,23 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
     }
 }
 
-// both norms the usual ones: RMS with weights alone
-bool lean(const Args &a) {
-    return a.post == ECHO_NORM_RMS && a.pre == ECHO_NORM_RMS && a.post_w && a.pre_w && !a.post_b && !a.pre_b &&
-           a.weight_offset == 0.f && a.block.data && a.residual.data && a.y.data;
+// Which of the usual pairs the norms are: both RMS with weights alone, or both LAYER with
+// weights and biases
+Lean lean(const Args &a) {
+    if (!a.post_w || !a.pre_w || a.weight_offset != 0.f || !a.block.data || !a.residual.data || !a.y.data) return Lean::No;
+    if (a.post == ECHO_NORM_RMS && a.pre == ECHO_NORM_RMS && !a.post_b && !a.pre_b) return Lean::Rms;
+    if (a.post == ECHO_NORM_LAYER && a.pre == ECHO_NORM_LAYER && a.post_b && a.pre_b) return Lean::Layer;
+    return Lean::No;
 }
 
-template <typename T, int WAVES, int V, bool BF, Width W, bool LEAN = false>
+template <typename T, int WAVES, int V, bool BF, Width W, Lean LEAN = Lean::No>
 hipError_t launch(const Args &a, hipStream_t st) {
-    if constexpr (!LEAN && BF && W == Width::Whole && V <= 2)
-        if (lean(a)) return launch<T, WAVES, V, BF, W, true>(a, st);
+    if constexpr (LEAN == Lean::No && W == Width::Whole) {
+        const Lean usual = lean(a);
+        if (usual == Lean::Rms) return launch<T, WAVES, V, BF, W, Lean::Rms>(a, st);
+        if constexpr (sizeof(T) == 8)
+            if (usual == Lean::Layer) return launch<T, WAVES, V, BF, W, Lean::Layer>(a, st);
+    }
     constexpr int kThreads = WAVES == 1 ? 256 : 64 * WAVES;
     constexpr int64_t kMost = ((int64_t)1 << 31) / kThreads;   // a launch has fewer than 2^32 threads
     const int64_t grid = WAVES == 1 ? ((int64_t)a.rows + 3) / 4 : a.rows;

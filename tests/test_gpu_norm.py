@@ -108,14 +108,17 @@ def test_forms(T, H, kw, gate, block, residual):
 
 
 @pytest.mark.parametrize("ty", ["bf16", "i8"])
-@pytest.mark.parametrize("H", [8, 16, 512, 1000, 2048, 2056, 4096, 4104, 8192])
-def test_two_rms_norms_in_bf16(H, ty):
-    """The usual pair of norms, few rows and many."""
+@pytest.mark.parametrize("H", [8, 16, 512, 520, 1000, 2048, 2056, 2560, 4096, 4104, 8192, 8200, 16384])
+@pytest.mark.parametrize("stream", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_the_usual_pairs_of_norms(H, ty, stream, kind):
+    """Two RMS norms, two LAYER norms with biases; few rows and many."""
     g = np.random.default_rng(H + 1)
-    say(f"[case] two RMS norms of {H} to {ty}")
-    for T, gate, pad in [(3, None, 0), (4, "channel", 8), (600, "token", 0)]:
-        _case(g, T, H, dict(post="rms", pre="rms", post_weight=True, pre_weight=True, block_scale=0.5),
-              ("bf16", "bf16", "bf16" if T != 3 else None, ty, "bf16"), gate=gate, pad=pad)
+    say(f"[case] two {kind} norms of {H} to {ty}, the stream in {stream}")
+    more = dict(post_bias=True, pre_bias=True) if kind == "layer" else {}
+    for T, gate, pad in [(3, None, 0), (4, "channel", 8), (600 if H < 8200 else 520, "token", 0)]:
+        _case(g, T, H, dict(post=kind, pre=kind, post_weight=True, pre_weight=True, block_scale=0.5, **more),
+              ("bf16", stream, stream if T != 3 else None, ty, "bf16"), gate=gate, pad=pad)
 
 
 @pytest.mark.parametrize("H", [48, 4096])
