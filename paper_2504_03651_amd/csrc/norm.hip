@@ -505,11 +505,10 @@ Lean lean(const Args &a) {
 
 template <typename T, int WAVES, int V, bool BF, Width W, Lean LEAN = Lean::No>
 hipError_t launch(const Args &a, hipStream_t st) {
-    if constexpr (LEAN == Lean::No && W == Width::Whole) {
+    if constexpr (LEAN == Lean::No && W != Width::Tiny) {
         const Lean usual = lean(a);
         if (usual == Lean::Rms) return launch<T, WAVES, V, BF, W, Lean::Rms>(a, st);
-        if constexpr (sizeof(T) == 8)
-            if (usual == Lean::Layer) return launch<T, WAVES, V, BF, W, Lean::Layer>(a, st);
+        if (usual == Lean::Layer) return launch<T, WAVES, V, BF, W, Lean::Layer>(a, st);
     }
     constexpr int kThreads = WAVES == 1 ? 256 : 64 * WAVES;
     constexpr int64_t kMost = ((int64_t)1 << 31) / kThreads;   // a launch has fewer than 2^32 threads

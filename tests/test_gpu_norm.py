@@ -108,7 +108,7 @@ def test_forms(T, H, kw, gate, block, residual):
 
 
 @pytest.mark.parametrize("ty", ["bf16", "i8"])
-@pytest.mark.parametrize("H", [8, 16, 512, 520, 1000, 2048, 2056, 2560, 4096, 4104, 8192, 8200, 16384])
+@pytest.mark.parametrize("H", [8, 9, 16, 512, 520, 1001, 2048, 2056, 2730, 4095, 4096, 4104, 8191, 8200, 16383, 16384])
 @pytest.mark.parametrize("stream", ["bf16", "f32"])
 @pytest.mark.parametrize("kind", ["rms", "layer"])
 def test_the_usual_pairs_of_norms(H, ty, stream, kind):
