@@ -202,16 +202,17 @@ __device__ __forceinline__ double inverse_root(double x) {
 
 // A row for WAVES waves (1: four rows a workgroup), V times eight values a lane, held
 // in registers from the first step to the last: one pass over memory, which bounds rows
-// in fp32 (1,003 rows of 2730, layer norms, 38 MB: 9.7 us, 4.0 TB/s, four sums one after
+// in fp32 (1,003 rows of 2730, layer norms, 38 MB: 8.9 us, 4.3 TB/s, four sums one after
 // the other on the way).  Rows that end in codes are bound by instructions as well, some
-// 24 in fp64 a value: 4,640 rows of 4096 with a gate, 133 MB, take 31.4 us, 4.2 TB/s, the
+// 24 in fp64 a value: 4,640 rows of 4096 with a gate, 133 MB, take 32.4 us, 4.1 TB/s, the
 // vector units busy two thirds of it.  LEAN: two RMS norms with weights, or two LAYER
 // norms with weights and biases, and no branches for all else, which cost copies of
 // registers between them (4,640 rows of two RMS norms: 41 us without; 3,937 of 6936 with
 // the stream in fp32 104, 73 with).  T: what sums and rows are held in.
 // The last eight of a row begin at H - 8, whatever H is a multiple of: what a lane
 // before them has too counts for that one alone (`skip`), and comes out the same, to be
-// written twice.  In rows of whole eights lanes behind the end hold zeros.  Where V <= 2 every input is asked for before the first sum.
+// written twice.  In rows of whole eights lanes behind the end hold zeros.  Where V <= 2
+// every input is asked for before the first sum.
 template <typename T, int WAVES, int V, bool BF, Width W, Lean LEAN>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V == 1 && (BF || WAVES < 8) ? 8 : 1) void join_kernel(Args a, uint32_t first) {
     constexpr bool USUAL = LEAN != Lean::No;
