@@ -293,12 +293,20 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
                 for (int i = 0; i < 8; ++i) x[u][i] = behind(u) ? T(0) : x[u][i] - mean;
         }
     };
-    auto squares = [&] {   // of this lane
+    // Of this lane.  What is another's, or behind the end (there an infinite gate or weight
+    // of the last eight leaves NaN), is left out, not multiplied by 0.
+    auto squares = [&] {
         T ss = T(0);
 #pragma unroll
-        for (int u = 0; u < V; ++u)
+        for (int u = 0; u < V; ++u) {
+            const T before = ss;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fma(x[u][i], mine(u, i) ? x[u][i] : T(0), ss);
+            for (int i = 0; i < 8; ++i) {
+                const T v = mine(u, i) ? x[u][i] : T(0);
+                ss = fma(v, v, ss);
+            }
+            if (behind(u)) ss = before;
+        }
         return ss;
     };
     auto inverse = [&](T ss, float eps) { return inverse_root(fma(ss, (T)a.inv_h, (T)eps)); };
