@@ -197,7 +197,8 @@ __device__ __forceinline__ float inverse_root(float x) { return rsqrtf(x); }
 // v_rsq_f64 is good to 2^-24 and better; one step of third order leaves 2^-70 of that
 __device__ __forceinline__ double inverse_root(double x) {
     const double y = __builtin_amdgcn_rsq(x), e = __builtin_fma(-x * y, y, 1.0);
-    return __builtin_fma(y * e, __builtin_fma(e, 0.375, 0.5), y);
+    const double root = __builtin_fma(y * e, __builtin_fma(e, 0.375, 0.5), y);
+    return x < __builtin_inf() ? root : y;   // of an infinity 0, of a NaN one
 }
 
 // A row for WAVES waves (1: four rows a workgroup), V times eight values a lane, held

@@ -57,3 +57,30 @@ def test_infinities_before_the_second_norm(H, post, ty):
             assert np.array_equal(s[~rows], s0[~rows]) and np.array_equal(y[~rows], y0[~rows])
             assert np.array_equal(s[rows][:, ~cols], s0[rows][:, ~cols]) and np.isinf(s[rows][:, cols]).all()
             assert (y[rows][:, ~cols] == 0).all() and np.isnan(y[rows][:, cols]).all()
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32", "i8"])
+@pytest.mark.parametrize("weights", [True, False])
+@pytest.mark.parametrize("H", WIDTHS)
+def test_infinities_before_the_first_norm(H, weights, ty):
+    """The block's norm is 0 but for one column: the sum is the residual there."""
+    g = np.random.default_rng(H)
+    T, hit = 5, 2
+    x = {n: IO.bf16(g.standard_normal((T, H))) for n in ("block", "residual", "gate")}
+    kw = dict(post="rms", pre="rms")
+    if weights:
+        kw.update({n: (1 + 0.2 * g.standard_normal(H)).astype(np.float32) for n in ("post_weight", "pre_weight")})
+    s0, y0, q0 = _join(x, H, kw, ty, T)
+    rows = np.arange(T) == hit
+    for at in sorted({0, max(H - 5, 0), H - 1}):
+        say(f"[case] an infinity in the block, column {at} of {H}, to {ty}")
+        x1 = {n: v.copy() for n, v in x.items()}
+        x1["block"][hit, at] = -np.inf
+        s, y, q = _join(x1, H, kw, ty, T)
+        cols = np.arange(H) == at
+        assert np.array_equal(s[~rows], s0[~rows]) and np.array_equal(y[~rows], y0[~rows])
+        assert np.array_equal(s[hit, ~cols], x["residual"][hit, ~cols]) and np.isnan(s[hit, at])
+        if ty == "i8":
+            assert np.isnan(q[hit]) and (y[hit] == 0).all() and np.array_equal(q[~rows], q0[~rows])
+        else:
+            assert np.isnan(y[hit]).all()
