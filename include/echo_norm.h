@@ -10,7 +10,10 @@
  *   RMS    x / sqrt(mean(x^2) + eps) * weight (+ bias)
  *   LAYER  (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * weight (+ bias).
  * Rows are held in fp32 from the first to the last step: y is the norm of the sum
- * before it is rounded to its type.  Where y is int8 codes they are those of
+ * before it is rounded to its type.  A norm's squares and mean may leave fp32's range
+ * where its input does not (rows above 1e19, or below 1e-19 without eps): such rows are
+ * taken times a power of two.  An infinity makes a LAYER norm's row NaN; of an RMS norm's
+ * row it leaves 0, and NaN in its own column.  Where y is int8 codes they are those of
  * echo_int8.h's rule for y in 64 bits (scale = fp32(amax / 127), 1 where that is 0,
  * code = y / scale to the nearest integer), and every step is taken in 64 bits, so
  * that codes next to a border do not hang on the order of sums.
