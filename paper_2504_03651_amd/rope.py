@@ -72,6 +72,11 @@ class Rope:
             refuse(where, f"frequencies has shape {tuple(self.frequencies.shape)}, not {(rotary_dim // 2,)}")
         self.magnitude = float(m.value if magnitude is None else magnitude)
 
+    def __setstate__(self, state):
+        """Of a copy, in this process or another: its description has an address of its own."""
+        self.__dict__.update(state)
+        self.at = ctypes.addressof(self.c)
+
 
 def rotate(rope: Rope, positions, q, k=None, q_out=None, k_out=None, inverse: bool = False,
            stream=None) -> None:

@@ -1,0 +1,33 @@
+"""What the bindings' objects point at stays theirs when they are copied."""
+import copy
+import ctypes
+import gc
+import pickle
+
+import pytest
+
+from paper_2504_03651_amd import norm, rope
+
+
+@pytest.mark.parametrize("how", [copy.copy, copy.deepcopy, lambda r: pickle.loads(pickle.dumps(r))])
+def test_a_copied_rope_points_at_its_own_description(how):
+    """The library is handed the address of a copy's own echo_rope_t, which is that of the
+    original only where they share it."""
+    import torch
+    first = rope.Rope(96, 32, layout="interleaved", theta=500000.0, device="cpu")
+    r = how(first)
+    assert r.at == ctypes.addressof(r.c)
+    want = bytes(first.c)
+    del first
+    gc.collect()
+    assert ctypes.string_at(r.at, ctypes.sizeof(rope.CRope)) == want
+    assert torch.equal(r.frequencies, rope.Rope(96, 32, theta=500000.0, device="cpu").frequencies)
+
+
+def test_a_norms_pointers_are_not_copied_away_from_their_tensors():
+    n = norm.Norm(64, pre="rms")
+    for how in (copy.deepcopy, pickle.dumps):
+        with pytest.raises(ValueError, match="pointers"):
+            how(n)
+    again = copy.copy(n)
+    assert again.c is n.c and again.at == ctypes.addressof(n.c)
