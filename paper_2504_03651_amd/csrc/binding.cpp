@@ -59,7 +59,7 @@ void axes(const char *where, const char *name, const at::Tensor &t, int64_t n) {
     if (t.dim() != n) refuse(where, std::string(name) + " has " + std::to_string(t.dim()) + " axes");
 }
 
-enum Types { kF32 = 1, kBf16 = 2, kI8 = 4, kI32 = 8, kReal = kF32 | kBf16 };
+enum Types { kF32 = 1, kBf16 = 2, kI8 = 4, kI32 = 8, kF64 = 16, kReal = kF32 | kBf16 };
 
 int type_of(const at::Tensor &t) {
     switch (t.scalar_type()) {
@@ -67,6 +67,7 @@ int type_of(const at::Tensor &t) {
         case at::kBFloat16: return kBf16;
         case at::kChar: return kI8;
         case at::kInt: return kI32;
+        case at::kDouble: return kF64;
         default: return 0;
     }
 }
@@ -77,9 +78,13 @@ void placed(const char *where, const char *name, const at::Tensor &t, int dev) {
                           (t.is_cuda() ? ", the current device is cuda:" + std::to_string(dev) : ", not on a GPU"));
 }
 
+void typed(const char *where, const char *name, const at::Tensor &t, int types) {
+    if (!(type_of(t) & types)) refuse(where, std::string(name) + " has dtype " + c10::toString(t.scalar_type()));
+}
+
 // the type and the place that every tensor is checked for
 void like(const char *where, const char *name, const at::Tensor &t, int types, int dev) {
-    if (!(type_of(t) & types)) refuse(where, std::string(name) + " has dtype " + c10::toString(t.scalar_type()));
+    typed(where, name, t, types);
     placed(where, name, t, dev);
 }
 
@@ -261,6 +266,10 @@ PyObject *rotate(PyObject *, PyObject *const *a, Py_ssize_t n) {
         axes(where, "q", q, 3);
         const int64_t T = q.size(0), D = rope->head_dim;
         sizes(where, {T});
+        // what the library reads R / 2 numbers of 64 bits of (its place: below)
+        shaped(where, "rope.frequencies", f, {rope->rotary_dim / 2});
+        typed(where, "rope.frequencies", f, kF64);
+        if (!f.is_contiguous()) refuse(where, "rope.frequencies is not contiguous");
         const int types = type_of(q) & kReal;
         if (a[5] == Py_None && a[7] != Py_None) refuse(where, "k_out without k");
         echo_rope_heads_t t[2];

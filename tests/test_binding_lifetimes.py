@@ -6,7 +6,7 @@ import pickle
 
 import pytest
 
-from paper_2504_03651_amd import norm, rope
+from paper_2504_03651_amd import echo, norm, rope
 
 
 @pytest.mark.parametrize("how", [copy.copy, copy.deepcopy, lambda r: pickle.loads(pickle.dumps(r))])
@@ -31,3 +31,31 @@ def test_a_norms_pointers_are_not_copied_away_from_their_tensors():
             how(n)
     again = copy.copy(n)
     assert again.c is n.c and again.at == ctypes.addressof(n.c)
+
+
+def _ropes():
+    import torch
+    r = rope.Rope(64, device="cpu")
+    f = r.frequencies
+    for freq, what in [(f.float(), "dtype"), (f[:16].clone(), "shape"), (f[None], "shape"),
+                       (torch.stack([f, f], 1)[:, 0], "not contiguous")]:
+        r.frequencies = freq
+        yield r, what
+
+
+def test_rotate_refuses_frequencies_of_another_type_or_length():
+    """They are read as R / 2 numbers of 64 bits."""
+    import torch
+    for r, what in _ropes():
+        with pytest.raises(echo.EchoError, match="rope.frequencies.*" + what):
+            rope.rotate(r, torch.zeros(4, dtype=torch.int32), torch.zeros(4, 2, 64))
+
+
+@pytest.mark.gpu
+def test_rotate_refuses_them_on_the_gpu():
+    import torch
+    for r, what in _ropes():
+        r.frequencies = r.frequencies.cuda() if what != "not contiguous" else torch.ones(32, 2, dtype=torch.float64,
+                                                                                         device="cuda")[:, 0]
+        with pytest.raises(echo.EchoError, match="rope.frequencies.*" + what):
+            rope.rotate(r, torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, 2, 64, device="cuda"))
