@@ -41,7 +41,8 @@ def _lib():
 class Norm:
     """The norms ``post`` (behind a block) and ``pre`` (before the next), each "none",
     "rms" or "layer", and the scales of residual and block (echo_norm_t).  Weights and
-    biases [hidden] are bf16 or fp32, all alike, or None: 1 and 0."""
+    biases [hidden] are bf16 or fp32, all alike, or None: 1 and 0.  They are read at each
+    call, in the memory that they have now."""
 
     def __init__(self, hidden: int, post: str = "none", pre: str = "none", post_weight=None,
                  post_bias=None, pre_weight=None, pre_bias=None, post_eps: float = 1e-5,
@@ -52,7 +53,8 @@ class Norm:
             if kind not in KINDS:
                 raise echo.EchoError(echo.ECHO_E_UNSUPPORTED, where, f"norm {kind!r}")
         sizes(where, hidden)
-        self.t = (post_weight, post_bias, pre_weight, pre_bias)   # kept alive
+        # kept alive, also where a parameter is given another tensor later
+        self.t = tuple(t if t is None else t.detach() for t in (post_weight, post_bias, pre_weight, pre_bias))
         given = [t for t in self.t if t is not None]
         self.device = given[0].get_device() if given else None
         if self.device is not None and self.device < 0:

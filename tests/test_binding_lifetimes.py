@@ -1,4 +1,5 @@
-"""What the bindings' objects point at stays theirs when they are copied."""
+"""What the bindings' objects point at stays theirs when they are copied, or their weights'
+owners are given others."""
 import copy
 import ctypes
 import gc
@@ -31,6 +32,20 @@ def test_a_norms_pointers_are_not_copied_away_from_their_tensors():
             how(n)
     again = copy.copy(n)
     assert again.c is n.c and again.at == ctypes.addressof(n.c)
+
+
+@pytest.mark.gpu
+def test_weights_stay_those_that_a_norm_was_made_with():
+    """A parameter that is given another tensor lets go of its memory; the norm does not."""
+    import torch
+    H = 4096
+    w = torch.nn.Parameter(torch.full((H,), 2.0, device="cuda"))
+    n = norm.Norm(H, pre="rms", pre_weight=w, pre_eps=0.0)
+    x, y = torch.ones(3, H, device="cuda"), torch.empty(3, H, device="cuda")
+    w.data = torch.full((H,), 5.0, device="cuda")
+    other = [torch.full((H,), 7.0, device="cuda") for _ in range(64)]   # the memory, had it been let go
+    norm.join(n, None, x, y=y)
+    assert (y == 2).all() and len(other) == 64
 
 
 def _ropes():
