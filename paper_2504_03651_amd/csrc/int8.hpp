@@ -2,6 +2,7 @@
 #pragma once
 
 #include "fp8_tiled.hpp"
+#include "int8_cut.hpp"
 
 namespace echo {
 namespace int8 {
@@ -23,8 +24,6 @@ using fp8::u32x4;
 using fp8::wave_lds;
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kStep = 128;   // bytes of a row that a step of a product takes
 
 // What a product's kernel reads and writes.
 struct Product {
