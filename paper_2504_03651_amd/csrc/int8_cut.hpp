@@ -34,6 +34,8 @@ constexpr struct {
                   {k128x128, 128, 128, .59, 0, 3.75, 2.},    {k128x128two, 128, 128, .70, .85, 3.55, 1.7},
                   {k128x160, 128, 160, .72, 0, 3.5, 2.},     {k256x128, 256, 128, .77, 0, 3.7, 2.},
                   {k256x192, 256, 192, 1.15, 0, 4., 3.4}};
+// (sums of ranges in tiles of 256 x 192 would spill registers)
+constexpr bool in_ranges(Form f) { return f != k256x192; }
 constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16};
 
 // Products of more tiles, or whose parts would take more, are not cut into ranges of K,
@@ -55,7 +57,7 @@ inline size_t most_parts_bytes(int T, int N, int K) {
     int64_t rows = 0;   // s times the tokens
     for (const auto &f : kTileForms) {
         const int m = kRangeTiles / cuts(N, f.n);
-        if (m > 1 && s_most > 1) rows = std::max(rows, std::min((int64_t)std::min(s_most, m) * T, (int64_t)m * f.t));
+        if (m > 1 && s_most > 1 && in_ranges(f.form)) rows = std::max(rows, std::min((int64_t)std::min(s_most, m) * T, (int64_t)m * f.t));
     }
     return std::min<size_t>((size_t)rows * pitch_of(N) * 4, kPartBytes);
 }
@@ -91,7 +93,7 @@ inline Cut cut_of(int T, int N, int K, bool f32) {
         if ((f.t > 32 && T <= f.t / 3) || (f32 && (f.form == k128x128two || f.form == k256x192))) continue;
         for (int s : kRanges) {
             const int64_t all = (int64_t)cuts(N, f.n) * cuts(T, f.t) * s;
-            if (s > 1 && (f.form == k256x192 || 2 * s > KB || all > kRangeTiles || parts_bytes(s, T, N) > kPartBytes)) break;
+            if (s > 1 && (!in_ranges(f.form) || 2 * s > KB || all > kRangeTiles || parts_bytes(s, T, N) > kPartBytes)) break;
             const int64_t each = (all + 255) / 256;   // of a CU
             const double one = f.form == k128x160 && T <= 160 ? .62 : f.one;   // waves of 16 x 160
             const double turns = f.two > 0 ? (double)(each / 2) * f.two + (double)(each % 2) * one

@@ -28,6 +28,12 @@ def test_the_workspace_holds_the_parts_of_every_smaller_batch():
         assert one[3] <= one[4] <= all_[4]
 
 
+def test_tiles_that_are_never_cut_ask_for_no_workspace():
+    """Those of 256 x 192: the most is that of 256 x 128, in 2,048 tiles."""
+    for N, K in [(28672, 4096), (20000, 8192), (14000, 2048)]:
+        assert int8.gemm_workspace_bytes(10 ** 6, N, K) == 2048 // -(-N // 256) * 128 * N * 4 < 256 << 20
+
+
 def test_every_cut_has_a_case():
     """Forms, variants and ranges of 300,000 sizes."""
     cases = [(t, n, k, f) for t, n, k in SIZES for f in (0, 1)] + S.FORMS
