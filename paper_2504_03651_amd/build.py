@@ -28,8 +28,34 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
 BINDING = os.path.join(PKG, "_binding.so")
 
 
-def build_binding(verbose: bool = False) -> str:
-    """The compiled part of the Python bindings (host code only), against PyTorch's headers."""
+def _lacking() -> str | None:
+    """What the compiled part of the bindings needs and is not here."""
+    import shutil
+    import sysconfig
+    cxx = os.environ.get("CXX", "g++")
+    if not shutil.which(cxx):
+        return f"the host compiler {cxx}"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python.h"
+    try:
+        import torch
+    except ImportError:
+        return "PyTorch"
+    header = os.path.join(os.path.dirname(torch.__file__), "include", "torch", "csrc", "autograd", "python_variable.h")
+    return None if os.path.exists(header) else "PyTorch's headers"
+
+
+def build_binding(verbose: bool = False) -> str | None:
+    """The compiled part of the Python bindings (host code only), against PyTorch's headers.
+    The library itself needs neither those nor a host compiler: without them there is no
+    such part, and the bindings that need it raise."""
+    lacking = _lacking()
+    if lacking:
+        if os.path.exists(BINDING):
+            os.remove(BINDING)
+        sys.stderr.write(f"{os.path.basename(BINDING)} is not built, {lacking} is missing: "
+                         "int8.py, rope.py and norm.py will raise\n")
+        return None
     import sysconfig
 
     import torch
