@@ -7,6 +7,7 @@
 #include "echo_fp8.h"
 #include "fp8.hpp"
 #include "fp8_stream.hpp"
+#include "rows.hpp"
 #include "status.hpp"
 
 namespace echo {
@@ -25,38 +26,10 @@ namespace fp8 {
 // indices 54), a matrix of 117 million in blocks of 128 x 128 68 (101); fp32 ones 62
 // and 104 us, 5.4 and 5.6 TB/s.
 
-// Eight values as they lie in memory
+// Eight values and their codes
 template <bool F32>
-struct Eight {
-    u32x4 a[F32 ? 2 : 1];
-    __device__ __forceinline__ void load(const void *x, int64_t e) {
-        const u32x4 *q = (const u32x4 *)((const uint8_t *)x + e * (F32 ? 4 : 2));
-#pragma unroll
-        for (int i = 0; i < (F32 ? 2 : 1); ++i) a[i] = q[i];
-    }
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int i = 0; i < (F32 ? 2 : 1); ++i) a[i] = (u32x4){0u, 0u, 0u, 0u};
-    }
-    __device__ __forceinline__ float get(int i) const {
-        if constexpr (F32) return __uint_as_float(a[i / 4][i % 4]);
-        return __uint_as_float(i & 1 ? a[0][i / 2] & 0xFFFF0000u : a[0][i / 2] << 16);
-    }
-    // bits of the largest magnitude, as fp32: above infinity's with a NaN
-    __device__ __forceinline__ uint32_t top() const {
-        if constexpr (F32) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m = max(m, a[i / 4][i % 4] & 0x7FFFFFFFu);
-            return m;
-        }
-        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-        u16x2 m = {0, 0};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, a[0][i] & 0x7FFF7FFFu));
-        return (uint32_t)max(m[0], m[1]) << 16;
-    }
+struct Eight : echo::Eight<F32> {
+    using echo::Eight<F32>::get;
     // the largest magnitude of those that are no NaN
     __device__ __forceinline__ float amax() const {
         float m = 0.f;

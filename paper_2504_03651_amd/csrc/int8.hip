@@ -173,11 +173,11 @@ hipError_t launch_rows(const Product &p, hipStream_t st) {
     }
 }
 
-template <bool F32, int BN, int BT, int WN, int WT, int STEP, int S>
+template <bool F32, int BN, int BT, int WN, int WT, int S>
 hipError_t launch_tiles(const Product &p, int ranges, hipStream_t st) {
     if constexpr (BT <= 64)
-        if (p.T <= BT) return launch_tiled<F32, true, BN, BT, WN, WT, STEP, S>(p, ranges, st);
-    return launch_tiled<F32, false, BN, BT, WN, WT, STEP, S>(p, ranges, st);
+        if (p.T <= BT) return launch_tiled<F32, true, BN, BT, WN, WT, S>(p, ranges, st);
+    return launch_tiled<F32, false, BN, BT, WN, WT, S>(p, ranges, st);
 }
 
 template <bool F32>
@@ -186,21 +186,21 @@ hipError_t launch_gemm(const Product &p, Cut c, hipStream_t st) {
     switch (c.form) {
         case kRows16: return launch_rows<F32, 1>(p, st);
         case kRows32: return launch_rows<F32, 2>(p, st);
-        case k64x32: e = launch_tiles<F32, 64, 32, 4, 1, 128, 6>(p, c.ranges, st); break;
-        case k64x64: e = launch_tiles<F32, 64, 64, 4, 1, 128, 4>(p, c.ranges, st); break;
-        case k128x64: e = launch_tiles<F32, 128, 64, 4, 1, 128, 3>(p, c.ranges, st); break;
-        case k128x96: e = launch_tiles<F32, 128, 96, 4, 2, 128, 4>(p, c.ranges, st); break;
-        case k128x128: e = launch_tiles<F32, 128, 128, 4, 2, 128, 4>(p, c.ranges, st); break;
+        case k64x32: e = launch_tiles<F32, 64, 32, 4, 1, 6>(p, c.ranges, st); break;
+        case k64x64: e = launch_tiles<F32, 64, 64, 4, 1, 4>(p, c.ranges, st); break;
+        case k128x64: e = launch_tiles<F32, 128, 64, 4, 1, 3>(p, c.ranges, st); break;
+        case k128x96: e = launch_tiles<F32, 128, 96, 4, 2, 4>(p, c.ranges, st); break;
+        case k128x128: e = launch_tiles<F32, 128, 128, 4, 2, 4>(p, c.ranges, st); break;
         case k128x160:   // one tile of tokens: a wave's sixteen weight rows against all of them
                          // (137 x 4096 x 14336 in eight ranges: 18.9 us, by 4 x 2 waves 20.2)
-            e = p.T <= 160 ? launch_tiles<F32, 128, 160, 8, 1, 128, 4>(p, c.ranges, st)
-                           : launch_tiles<F32, 128, 160, 4, 2, 128, 4>(p, c.ranges, st);
+            e = p.T <= 160 ? launch_tiles<F32, 128, 160, 8, 1, 4>(p, c.ranges, st)
+                           : launch_tiles<F32, 128, 160, 4, 2, 4>(p, c.ranges, st);
             break;
-        case k256x128: e = launch_tiles<F32, 256, 128, 4, 2, 128, 3>(p, c.ranges, st); break;
+        case k256x128: e = launch_tiles<F32, 256, 128, 4, 2, 3>(p, c.ranges, st); break;
         default:   // fp32 results of these tiles would spill registers: not chosen
             if constexpr (F32) e = hipErrorInvalidValue;
-            else if (c.form == k128x128two) e = launch_tiles<F32, 128, 128, 2, 2, 128, 2>(p, c.ranges, st);
-            else e = launch_tiles<F32, 256, 192, 4, 2, 128, 2>(p, c.ranges, st);
+            else if (c.form == k128x128two) e = launch_tiles<F32, 128, 128, 2, 2, 2>(p, c.ranges, st);
+            else e = launch_tiles<F32, 256, 192, 4, 2, 2>(p, c.ranges, st);
     }
     if (e != hipSuccess || c.ranges == 1 || (e = hipGetLastError()) != hipSuccess) return e;
     const int64_t n = (int64_t)p.T * (p.part_pitch / 4);

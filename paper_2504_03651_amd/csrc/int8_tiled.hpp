@@ -46,10 +46,10 @@ __device__ __forceinline__ void landed_but_stages(int left) {
 constexpr int scale_room(int BN, int BT) { return (2 * BN + BT + 63) / 64 * 64; }
 
 // LDS of a workgroup: two share a CU where it holds them
-constexpr int lds_bytes(int BN, int BT, int STEP, int S) { return S * (BN + BT) * STEP + 8 * scale_room(BN, BT); }
+constexpr int lds_bytes(int BN, int BT, int S) { return S * (BN + BT) * kStep + 8 * scale_room(BN, BT); }
 
-// One workgroup of WN x WT waves: BN weight rows by BT tokens, K in steps of STEP (64
-// or 128) through a ring of S LDS stages that are filled straight from memory.  A row's
+// One workgroup of WN x WT waves: BN weight rows by BT tokens, K in steps of 128
+// through a ring of S LDS stages that are filled straight from memory.  A row's
 // 16-byte pieces lie in an order that turns with the row, so that the lanes that read
 // one piece of neighbouring rows meet different banks.  A step's operands are read into
 // registers as the matrix instructions of the step before are done with theirs: a stage
@@ -68,21 +68,21 @@ constexpr int lds_bytes(int BN, int BT, int STEP, int S) { return S * (BN + BT) 
 // TB/s in the place of 20); instructions of 32 x 32 x 32 (products alone 12% slower); four
 // waves of 128 x 128 spill; workgroups that start apart, so that one's results meet others'
 // products, 3% at best.
-template <bool F32, bool ONCE, int BN, int BT, int WN, int WT, int STEP, int S>
-__global__ __launch_bounds__(64 * WN * WT, WN * WT * (2 * lds_bytes(BN, BT, STEP, S) <= 160 * 1024 ? 2 : 1) / 4) void tiled_kernel(Product p, Units u) {
+template <bool F32, bool ONCE, int BN, int BT, int WN, int WT, int S>
+__global__ __launch_bounds__(64 * WN * WT, WN * WT * (2 * lds_bytes(BN, BT, S) <= 160 * 1024 ? 2 : 1) / 4) void tiled_kernel(Product p, Units u) {
     constexpr int W = WN * WT, NW = BN / WN, TW = BT / WT;   // a wave's rows and tokens
-    constexpr int NI = NW / 16, NJ = TW / 16, NH = STEP / 64;
-    constexpr int STAGE = (BN + BT) * STEP;
+    constexpr int NI = NW / 16, NJ = TW / 16, NH = kStep / 64;
+    constexpr int STAGE = (BN + BT) * kStep;
     constexpr int PIECES = STAGE / 1024;                     // 1 KiB copies of a stage
     constexpr int COPIES = (PIECES + W - 1) / W, EXTRA = PIECES % W;
-    constexpr int RC = 1024 / STEP, PR = STEP / 16;          // rows of a copy, pieces of a row
+    constexpr int RC = 1024 / kStep, PR = kStep / 16;        // rows of a copy, pieces of a row
     // the epilogue: sums of ROWS tokens and CP columns of each wave at a time; E columns
     // and Q lanes of a row
     constexpr int E = F32 ? 4 : 8, ROOM = STAGE / W;
     constexpr int CP = NW % 64 == 0 && ROOM >= 4096 ? 64 : NW % 32 == 0 ? 32 : 16;
     // ranges of K, and a residual that is asked for early: where registers allow it
     constexpr bool CUTS = BN * BT <= 128 * 256;
-    constexpr bool REST = BN * BT * (F32 ? 2 : 1) <= 128 * 256 && (W <= 4 || 2 * lds_bytes(BN, BT, STEP, S) > 160 * 1024);
+    constexpr bool REST = BN * BT * (F32 ? 2 : 1) <= 128 * 256 && (W <= 4 || 2 * lds_bytes(BN, BT, S) > 160 * 1024);
     constexpr int Q = CP / E, ROWS = Q < 4 ? 64 / Q : 16, CHUNKS = CP / 4;
     static_assert(!ONCE || BN / RC % W == 0, "a copy is of weights in all waves or none");
     static_assert(STAGE % 1024 == 0 && BN % RC == 0 && NW % CP == 0 && TW % ROWS == 0 && S >= 2);
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(64 * WN * WT, WN * WT * (2 * lds_bytes(BN, BT, STEP
     const int wn = wave % WN, wt = wave / WN;
     const bool more = EXTRA == 0 || wave < EXTRA;
     // the place of piece q of row r: rows whose places start at the same bank differ
-    auto turn = [](int r) { return PR == 8 ? r & 7 : (r >> 1) & 3; };
+    auto turn = [](int r) { return r & (PR - 1); };
     const int piece = (lane % PR) ^ turn(lane / PR);
 
     const int xcd = blockIdx.x & 7, groups = (gridDim.x + 7 - xcd) / 8;
@@ -110,8 +110,8 @@ __global__ __launch_bounds__(64 * WN * WT, WN * WT * (2 * lds_bytes(BN, BT, STEP
         n0 = BN * at.ni;
         row0 = BT * at.ti;
         rows = min(BT, p.T - row0);
-        kb0 = (int)((int64_t)p.KB * range / u.ranges) * (kStep / STEP);
-        kb1 = (int)((int64_t)p.KB * (range + 1) / u.ranges) * (kStep / STEP);
+        kb0 = (int)((int64_t)p.KB * range / u.ranges);
+        kb1 = (int)((int64_t)p.KB * (range + 1) / u.ranges);
         wsrc = p.w + (int64_t)n0 * p.K;
         xsrc = p.x + (int64_t)row0 * p.K;
 #pragma unroll
@@ -124,8 +124,8 @@ __global__ __launch_bounds__(64 * WN * WT, WN * WT * (2 * lds_bytes(BN, BT, STEP
     // copy i of stage kb: a wave's own 1 KiB of it
     auto copy = [&](int kb, int slot, int i) {
         if (i + 1 == COPIES && !more) return;
-        const bool in = STEP * (kb + 1) <= p.K || STEP * kb + 16 * piece < p.K;
-        const uint8_t *from = (W * i + wave < BN / RC ? wsrc : xsrc) + (int64_t)STEP * kb + src[i];
+        const bool in = kStep * (kb + 1) <= p.K || kStep * kb + 16 * piece < p.K;
+        const uint8_t *from = (W * i + wave < BN / RC ? wsrc : xsrc) + (int64_t)kStep * kb + src[i];
         if (!in) from = kZeros;
         lds_void *to = (lds_void *)(lds + slot * STAGE + 1024 * (W * i + wave));
         if (ONCE && W * i < BN / RC) __builtin_amdgcn_global_load_lds((const void *)from, to, 16, 0, 2);   // 2: nt
@@ -166,10 +166,10 @@ __global__ __launch_bounds__(64 * WN * WT, WN * WT * (2 * lds_bytes(BN, BT, STEP
     u32x4 x[NJ], w[NI];   // the operands of 64 of K
     i32x4 acc[NI][NJ];
     auto read_x = [&](int slot, int h, int j) {
-        return *(const u32x4 *)(lds + slot * STAGE + (BN + wt * TW + 16 * j + c) * STEP + at[h]);
+        return *(const u32x4 *)(lds + slot * STAGE + (BN + wt * TW + 16 * j + c) * kStep + at[h]);
     };
     auto read_w = [&](int slot, int h, int i) {
-        return *(const u32x4 *)(lds + slot * STAGE + (wn * NW + 16 * i + c) * STEP + at[h]);
+        return *(const u32x4 *)(lds + slot * STAGE + (wn * NW + 16 * i + c) * kStep + at[h]);
     };
 
     int slot = 0;   // of the tile's first stage, then of the last one read
@@ -326,9 +326,9 @@ __global__ __launch_bounds__(64 * WN * WT, WN * WT * (2 * lds_bytes(BN, BT, STEP
     }
 }
 
-template <bool F32, bool ONCE, int BN, int BT, int WN, int WT, int STEP, int S>
+template <bool F32, bool ONCE, int BN, int BT, int WN, int WT, int S>
 hipError_t launch_tiled(const Product &p, int ranges, hipStream_t st) {
-    constexpr int bytes = lds_bytes(BN, BT, STEP, S);
+    constexpr int bytes = lds_bytes(BN, BT, S);
     static_assert(bytes <= 160 * 1024);
     static std::atomic<int> resident[64];
     Units u;
@@ -339,7 +339,7 @@ hipError_t launch_tiled(const Product &p, int ranges, hipStream_t st) {
     const int64_t all = (int64_t)u.n_tiles * u.t_tiles * ranges;
     u.all = (int)all;
     // workgroups beyond an XCD's units end at once
-    return launch_lds(tiled_kernel<F32, ONCE, BN, BT, WN, WT, STEP, S>, resident, bytes, bytes, (all + 7) / 8 * 8, true,
+    return launch_lds(tiled_kernel<F32, ONCE, BN, BT, WN, WT, S>, resident, bytes, bytes, (all + 7) / 8 * 8, true,
                       64 * WN * WT, st, p, u);
 }
 
