@@ -16,7 +16,10 @@
  * row it leaves 0, and NaN in its own column.  Where y is int8 codes they are those of
  * echo_int8.h's rule for y in 64 bits (scale = fp32(amax / 127), 1 where that is 0,
  * code = y / scale to the nearest integer), and every step is taken in 64 bits, so
- * that codes next to a border do not hang on the order of sums.
+ * that codes hang on the order of sums only within 2^-40 steps of a border.  That order
+ * goes by H alone where y is no codes: a row's results are the same in any batch.  Where it
+ * is, it goes by the number of rows as well (up to 512 and more), and sum, rounded from 64
+ * bits, may be a unit in the last place apart now and then.
  *
  * The conventions of echo.h hold: device pointers on the current device, work
  * enqueued on `stream`, nothing allocated, nothing kept, every check before

@@ -192,7 +192,7 @@ hipError_t launch_gemm(const Product &p, Cut c, hipStream_t st) {
         case k128x96: e = launch_tiles<F32, 128, 96, 4, 2, 4>(p, c.ranges, st); break;
         case k128x128: e = launch_tiles<F32, 128, 128, 4, 2, 4>(p, c.ranges, st); break;
         case k128x160:   // one tile of tokens: a wave's sixteen weight rows against all of them
-                         // (137 x 4096 x 14336 in eight ranges: 18.9 us, by 4 x 2 waves 20.2)
+                         // (137 x 4096 x 14336 in six ranges: 20.7 us, by 4 x 2 waves 21.1)
             e = p.T <= 160 ? launch_tiles<F32, 128, 160, 8, 1, 4>(p, c.ranges, st)
                            : launch_tiles<F32, 128, 160, 4, 2, 4>(p, c.ranges, st);
             break;

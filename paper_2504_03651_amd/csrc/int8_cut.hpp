@@ -63,18 +63,20 @@ inline size_t most_parts_bytes(int T, int N, int K) {
 }
 
 // The cut of least estimated time, in microseconds fitted to bf16 results of 430 sizes (T 1
-// to 4,640, N 64 to 28,672, K 128 to 14,336, weights from memory): 1.0% (geometric mean)
-// above the best cut of each, 24% at most (20 x 17342 x 8256, where four ranges of K would
-// be best); over 130 sizes with fp32 results 1.2% and 35% (54 x 5152 x 8080).
+// to 4,640, N 64 to 28,672, K 128 to 14,336, weights from memory).  In the 395 of them whose
+// cut was timed it is 1.2% (geometric mean) above the best cut of each, 38% at most (46 x 128
+// x 10912: 8.6 us, by 16 weight rows 6.5, whose price is too high where there are few of
+// them; then 24%, 20 x 17342 x 8256, 48 us, in four ranges of K 38); over 130 sizes with fp32
+// results 1.2% and 35% (54 x 5152 x 8080).
 //   Weights and tokens come at 5.0 TB/s at most.
 //   kRows: 16 or 32 weight rows a workgroup, every wave on its own; one workgroup a
-//   CU, which takes in 70 KB a microsecond, tokens among them (8 x 6144 x 4096: 7.2 by 32
-//   rows; 64 x 32 tiles take over where a CU has more than one: 8 x 10911 x 3056 14.4
-//   and 11.7).
+//   CU, which takes in 70 KB a microsecond, tokens among them (8 x 6144 x 4096, launches
+//   one after the other: 7.2 by 32 rows, 9.1 by 16; 64 x 32 tiles take over where a CU has
+//   more than one: 8 x 10911 x 3056 13.0, by 32 rows 14.3).
 //   k128x128two: four waves of 64 x 64, two workgroups a CU, so that one's results leave
-//   beside the other's products (1,847 x 26626 x 512 55 us, in tiles of 256 x 192 76, of
+//   beside the other's products (1,847 x 26626 x 512 53 us, in tiles of 256 x 192 73, of
 //   128 x 128 by eight waves, four stages and one workgroup a CU, which ranges of K and
-//   few tiles take, 78).
+//   few tiles take, 71).
 //   Ranges of K cost a second launch and their sums' way to memory and back.
 inline Cut cut_of(int T, int N, int K, bool f32) {
     const int KB = cuts(K, kStep);

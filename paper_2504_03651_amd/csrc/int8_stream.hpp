@@ -11,8 +11,8 @@ namespace int8 {
 // equal ranges of K and their sums meet in LDS.  A wave copies its 128 bytes of the
 // weight rows and of XR token rows straight into a ring of D stages of its own and
 // waits for nobody.  XR 8: at most 8 tokens, the operand's other columns repeat them.
-// Bound by memory and a launch: 8 x 6144 x 4096 takes 5.9 us with weights from the
-// caches, 6.4 with weights from memory (25 MB, 4.0 TB/s).
+// Bound by memory and a launch: 8 x 6144 x 4096 takes 6.1 us with weights from the
+// caches, 6.4 a call with weights from memory (25 MB, 4.0 TB/s).
 constexpr int kStreamWaves = 8;
 
 constexpr int stream_stage(int NT, int XR) { return (16 * NT + XR) * kStep; }

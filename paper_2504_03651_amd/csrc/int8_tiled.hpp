@@ -57,12 +57,12 @@ constexpr int lds_bytes(int BN, int BT, int S) { return S * (BN + BT) * kStep + 
 // the matrix instructions' accumulators to the end.
 // No more workgroups are launched than run at once: each goes on to a next tile, whose
 // first copies it starts before it writes the last one's results through one stage.
-// 4,640 x 28672 x 4096 in tiles of 256 x 192 takes 526 us, 2.07 PetaOp/s (a library's
+// 4,640 x 28672 x 4096 in tiles of 256 x 192 takes 532 us, 2.05 PetaOp/s (a library's
 // product of 8,192^3: 2.02): copies alone 374, products with their reads of LDS alone 345,
 // everything but the results 460.  Matrix instructions are busy 51% of the time at the
 // 1.97 GHz that the card then holds, three in four requests of the copies hit an XCD's
 // L2, LDS reads have no conflicts.  137 x 4096 x 14336, tiles of 128 x 160 in six ranges
-// of K: 20 us, 2.9 TB/s of weights, behind its copies.  What was tried: a step's copies
+// of K: 20.7 us, 2.8 TB/s of weights, behind its copies.  What was tried: a step's copies
 // asked for at once, ahead of its products, hold the waves up (two stages of 256 x 256:
 // 548 us and more); rows of 64 bytes halve what a request of the L2 brings (copies of 13
 // TB/s in the place of 20); instructions of 32 x 32 x 32 (products alone 12% slower); four

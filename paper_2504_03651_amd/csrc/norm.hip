@@ -21,8 +21,10 @@ using fp8::u32x2;
 using fp8::u32x4;
 
 // Codes of up to so many rows take a row by more waves of fewer values each, which has
-// the shorter way (8 rows of 4096: 5.4 us, by half the waves 7.4); past them what a wave
-// does once for its values weighs more (4,640 rows: 49 and 41 us).
+// the shorter way (8 rows of 2048, two LAYER norms, launches one after the other: 3.9 us,
+// by half the waves 5.0; 184 rows 4.3 and 5.4; two RMS norms of 8 rows of 4096 are the
+// other way round, 3.7 and 3.4); past them what a wave does once for its values weighs
+// more (4,640 rows of 4096: 39 and 32 us).
 constexpr int kFewRows = 512;
 
 struct Rows {
@@ -203,13 +205,13 @@ __device__ __forceinline__ double inverse_root(double x) {
 
 // A row for WAVES waves (1: four rows a workgroup), V times eight values a lane, held
 // in registers from the first step to the last: one pass over memory, which bounds rows
-// in fp32 (1,003 rows of 2730, layer norms, 38 MB: 8.9 us, 4.3 TB/s, four sums one after
-// the other on the way).  Rows that end in codes are bound by instructions as well, some
+// in fp32 (1,003 rows of 2730, layer norms, 38 MB: 9.6 us, 4.0 TB/s, four sums one after
+// the other on the way, those of the means in 64 bits).  Rows that end in codes are bound by instructions as well, some
 // 24 in fp64 a value: 4,640 rows of 4096 with a gate, 133 MB, take 32.4 us, 4.1 TB/s, the
 // vector units busy two thirds of it.  LEAN: two RMS norms with weights, or two LAYER
 // norms with weights and biases, and no branches for all else, which cost copies of
-// registers between them (4,640 rows of two RMS norms: 41 us without; 3,937 of 6936 with
-// the stream in fp32 104, 73 with).  T: what sums and rows are held in.
+// registers between them (4,640 rows of two RMS norms: 38 us without; 3,937 of 6936 with
+// the stream in fp32 98, 70 with; 1,003 rows of two layer norms 10.7, 9.6 with).  T: what sums and rows are held in.
 // The last eight of a row begin at H - 8, whatever H is a multiple of: what a lane
 // before them has too counts for that one alone (`skip`), and comes out the same, to be
 // written twice.  In rows of whole eights lanes behind the end hold zeros.  Where V <= 2
@@ -278,7 +280,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, sizeof(T) == 4 && V 
 
     T x[V][8];
     constexpr bool CODES = sizeof(T) == 8;
-    auto any = [](bool v) { return __builtin_expect_with_probability(__builtin_amdgcn_ballot_w64(v) != 0, false, 0.9); };   // of a row's, all alike
+    auto any = [](bool v) {   // of what all lanes of a row have alike, and rarely
+        return __builtin_expect_with_probability(__builtin_amdgcn_ballot_w64(v) != 0, false, 0.9);
+    };
     // In fp32 a row whose squares leave the range, or a difference from whose mean may, is
     // taken times 2^shift, which brings the larger of its largest value and the root of eps
     // to about 1, and which its norm does not depend on.  Rows with an infinity stay.
@@ -585,9 +589,9 @@ hipError_t launch(const Args &a, hipStream_t st) {
 
 // Sums in fp32 depend on how a row is spread over lanes, so that this goes by its width
 // alone; codes, which do not, take fewer waves of more values each where rows are many
-// (4,333 rows of 640: 11.8 us by one wave, by four of which a row fills a third 16.3).
-// Sixteen waves a row of up to 8192 were slower than eight (12 rows of 5264 5.8 and 5.2
-// us, 1,136 of 7062 in fp32 37.6 and 33.1).
+// (4,333 rows of 640: 11.2 us by one wave, by four of which a row fills a third 17.1).
+// Sixteen waves a row of up to 8192 were slower than eight (12 rows of 5264 into codes 5.9
+// and 5.4 us, 1,136 of 7062 into fp32 21.8 and 21.3).
 template <typename T, bool BF, Width W>
 hipError_t launch_by_width(const Args &a, hipStream_t st) {
     if (a.H <= 512) return launch<T, 1, 1, BF, W>(a, st);
